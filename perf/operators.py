@@ -7,9 +7,9 @@ taken on to the half format that the next layer reads.  The operators of
   gated           gated feed-forward: the stacked projections P = X W^T (gate rows of W, then up
                   rows), delivered in FP32 where ``deliver``, and H = act(P_gate) P_up.
   gated_narrow    H once more from a delivered (and repaired) P.
-  gated_grad      the gradient dP of P from that of H, as stored and transposed (the operands of the
-                  two products of the backward pass).
-  gated_products  those products, dX = dP W and dW = dP^T X, delivered in FP32.
+  gated_grad      the gradient dP of P from that of H; where ``deliver`` its transpose too, which is
+                  the first operand of dW when that product is verified.
+  gated_products  the products of the backward pass, dX = dP W and dW = dP^T X, delivered in FP32.
   adapters        low-rank adapters of many requests added to a shared projection's product C:
                   Y_i = C_i + scale_a (X_i A_a^T) B_a^T with a = index_i, none where it is -1.
   heads           norm of each query and key head of a QKV product with the position rotation;
@@ -129,8 +129,8 @@ def work(case):
         if kind == "gated_narrow":
             return {"bytes": 10 * t * f, "flops": 10 * t * f}
         if kind == "gated_grad":
-            return {"bytes": 18 * t * f, "flops": 20 * t * f}
-        return {"bytes": 8 * t * f + 2 * t * d + 4 * f * d + 4 * t * d + 8 * f * d,
+            return {"bytes": (18 if case["deliver"] else 14) * t * f, "flops": 20 * t * f}
+        return {"bytes": 4 * t * f + 2 * t * d + 4 * f * d + 4 * t * d + 8 * f * d,
                 "flops": 8 * t * d * f}
     if kind == "adapters":
         k, n, r = float(case["k"]), float(case["n"]), float(case["rank"])
@@ -178,7 +178,6 @@ def prepare(case, seed):
             st["dH"] = mat(t, f, std=0.05)
         if kind == "gated_products":
             st["dP"] = mat(t, 2 * f, std=0.05)
-            st["dPt"] = st["dP"].t().contiguous()
     elif kind == "adapters":
         k, n, r, count = case["k"], case["n"], case["rank"], case["count"]
         st["X"] = mat(t, k)
@@ -237,10 +236,10 @@ def _run_own(st):
     if kind == "gated_narrow":
         return {"H": fl.gated_narrow(st["P"], case["fmt"], act=case["act"])}
     if kind == "gated_grad":
-        dP, dPt = fl.gated_grad(st["dH"], st["P"], act=case["act"])
+        dP, dPt = fl.gated_grad(st["dH"], st["P"], act=case["act"], transpose=case["deliver"])
         return {"dP": dP, "dPt": dPt}
     if kind == "gated_products":
-        dX, dW = fl.gated_products(st["dP"], st["dPt"], st["X"], st["W"])
+        dX, dW = fl.gated_products(st["dP"], st["X"], st["W"])
         return {"dX": dX, "dW": dW}
     if kind == "adapters":
         return {"Y": fl.adapters(st["C"], st["X"], st["A"], st["B"], st["index"], st["scale"],
@@ -300,9 +299,9 @@ def _run_plain(st):
         if kind == "gated_grad":
             g, u, dH = st["P"][:, :f], st["P"][:, f:], st["dH"].float()
             dP = torch.cat((dH * u * _act_grad(g, act), dH * _act(g, act)), 1).to(h)
-            return {"dP": dP, "dPt": dP.t().contiguous()}
-        return {"dX": torch.mm(st["dP"].float(), st["W"].float()),
-                "dW": torch.mm(st["dPt"].float(), st["X"].float())}
+            return {"dP": dP, "dPt": dP.t().contiguous() if case["deliver"] else None}
+        dP = st["dP"].float()
+        return {"dX": torch.mm(dP, st["W"].float()), "dW": torch.mm(dP.t(), st["X"].float())}
     if kind == "adapters":
         # every row against every adapter, the columns of other adapters set to zero
         count, r, n = case["count"], case["rank"], case["n"]
@@ -379,7 +378,7 @@ def exact(case, seed):
         H = _exact_act(P.narrow(1, 0, f), act) * P.narrow(1, f, f)
         if kind == "gated_grad":
             (dP,) = torch.autograd.grad(H, P, st["dH"].double())
-            return {"dP": dP, "dPt": dP.t().contiguous()}
+            return {"dP": dP, "dPt": dP.t().contiguous() if case["deliver"] else None}
         if kind == "gated_narrow":
             return {"H": H}
         return {"H": H, "P": P if case["deliver"] else None}
