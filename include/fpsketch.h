@@ -325,6 +325,98 @@ fpsketch_status fpsketch_recalibrate_host(int64_t n1, int64_t n3, int32_t m, dou
  * III-G): finite samples only, magnitudes clipped at 64 x their median.  NaN if none. */
 double fpsketch_rms_hat_samples(const float* samples, int64_t count);
 
+/* ----------------------------------------------------------------------------------------- */
+/* Operators around a delivered product.                                                      */
+/*                                                                                            */
+/* A linear layer's product C = A W^T leaves its GEMM in FP32 to be verified and is narrowed   */
+/* afterwards.  These calls take it on together with the layer's own arithmetic, and deliver   */
+/* products of their own in FP32, in the layouts that fpsketch_probe, fpsketch_localize and    */
+/* fpsketch_apply take.                                                                        */
+/*                                                                                            */
+/* All of them: device pointers on the current device, which must be gfx950 (FPSK_ENODEV);     */
+/* dense row-major arrays, aligned to their elements (no more is needed; groups of 8 halves or */
+/* 4 floats per row on 16-byte boundaries are the fast case); `dtype` is the half format       */
+/* (FPSK_EDTYPE otherwise).  They only enqueue kernels on `stream`: no allocation, no host     */
+/* synchronization, no memset, so they can be captured.  Nothing is kept between calls, and    */
+/* results are the same bit for bit from call to call.  t = 0 is an empty batch: nothing is    */
+/* read, and nothing written but gradients that are sums over its rows, which are zero.        */
+/* Outputs and workspace overlap neither each other nor an input (FPSK_EINVAL).  `workspace`   */
+/* holds at least what the operator's _workspace function says for the same arguments (bytes;  */
+/* may be 0 and then NULL), aligned to 16 bytes; it belongs to the call until its work on      */
+/* `stream` is done, so calls that may overlap in time (other streams, graphs replayed beside  */
+/* each other) each need their own.  Sums, products and statistics are held in FP32 or more,   */
+/* and each result is rounded once.  FPSK_ESHAPE: a dimension outside [1, 2^31) (t: [0, 2^31)) */
+/* or an array of more than 2^40 elements; FPSK_EINVAL: null or misaligned pointers and the    */
+/* rest.                                                                                       */
+
+typedef enum { FPSK_SILU = 0, FPSK_GELU = 1, FPSK_GELU_TANH = 2 } fpsketch_act;
+typedef enum { FPSK_PAIRS_HALF = 0, FPSK_PAIRS_INTERLEAVED = 1 } fpsketch_pairs;
+
+/* Gated feed-forward: P = X W^T with X t x d and the stacked weight W 2f x d (f gate rows, then f
+ * up rows), and H = act(G) U (t x f, half format) with G = P[:, :f], U = P[:, f:], in one kernel.
+ * H is formed from the FP32 products.  P (t x 2f FP32) is delivered when not NULL: it is the C of
+ * a context (t, d, 2f, dtype) with b_layout 1 and B = W. */
+fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f,
+                               fpsketch_dtype dtype, fpsketch_act act, void* H, float* P,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+int64_t fpsketch_gated_workspace(int64_t t, int64_t d, int64_t f);
+
+/* H = act(G) U from a delivered product, for instance after fpsketch_apply repaired it; the same
+ * bits as fpsketch_gated gives for that P. */
+fpsketch_status fpsketch_gated_narrow(const float* P, int64_t t, int64_t f, fpsketch_dtype dtype,
+                                      fpsketch_act act, void* H, void* stream);
+
+/* The gradient of P from that of H (t x f, half format): dP = [dH U act'(G), dH act(G)] (t x 2f,
+ * half format).  dPt (2f x t), when not NULL, is its transpose: the A of a context (2f, t, d,
+ * dtype) that verifies dW. */
+fpsketch_status fpsketch_gated_grad(const void* dH, const float* P, int64_t t, int64_t f,
+                                    fpsketch_dtype dtype, fpsketch_act act, void* dP, void* dPt,
+                                    void* stream);
+
+/* The products of the backward pass, delivered in FP32: dX = dP W (t x d; a context (t, 2f, d)
+ * with B = W verifies it) and dW = dP^T X (2f x d).  Either may be NULL and is then left out. */
+fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const void* W, int64_t t,
+                                        int64_t d, int64_t f, fpsketch_dtype dtype, float* dX,
+                                        float* dW, void* workspace, int64_t workspace_bytes,
+                                        void* stream);
+int64_t fpsketch_gated_products_workspace(int64_t t, int64_t d, int64_t f);
+
+/* Low-rank adapters of many requests on a verified product C (t x n FP32) of the shared weight:
+ * Y_i = C_i + scale_a (X_i A_a^T) B_a^T with a = index_i, X t x k, A count x rank x k and
+ * B count x n x rank (rank 1 to 256; adapters of a smaller rank are padded with zeros).  index -1:
+ * no adapter, Y_i = C_i; any other index outside [0, count) makes the row NaN.  Y (t x n) is in
+ * the half format, or in FP32 with y_dtype FPSK_F32.  Rows of one adapter need not be neighbours.
+ * C is not modified, so that it can still be localized and repaired. */
+fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, const void* B,
+                                  const int32_t* index, const float* scale, int64_t t, int64_t k,
+                                  int64_t n, int32_t count, int32_t rank, fpsketch_dtype dtype,
+                                  void* Y, fpsketch_dtype y_dtype, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+int64_t fpsketch_adapters_workspace(int64_t t, int64_t k, int64_t n, int32_t count, int32_t rank);
+
+/* Heads of a QKV product C (t x (hq + 2 hkv) hd FP32: query, key, value heads of hd entries, hd
+ * at most 512): q (t x hq x hd), k and v (t x hkv x hd) in the half format.  Query and key heads
+ * are normed with the gains gq, gk (hd FP32 each; both NULL: no norm),
+ * x g / sqrt(mean x^2 + eps), then the first rd entries (even, at most hd) are rotated in pairs by
+ * pos_i freq_p, p < rd / 2: pairs (p, p + rd / 2), or (2p, 2p + 1) with FPSK_PAIRS_INTERLEAVED.
+ * Angles are formed and reduced in FP64.  pos and freq may be NULL when rd is 0. */
+fpsketch_status fpsketch_heads(const float* C, int64_t t, int32_t hq, int32_t hkv, int32_t hd,
+                               const float* gq, const float* gk, double eps, const int64_t* pos,
+                               const float* freq, int32_t rd, int32_t pairs, fpsketch_dtype dtype,
+                               void* q, void* k, void* v, void* stream);
+
+/* Its backward pass: dC (t x (hq + 2 hkv) hd, half format: the operand of the projection's own
+ * products) from dq, dk, dv (half format), and with gains dgq, dgk (hd FP32 each, summed over
+ * tokens and heads in a fixed order).  C is the product the heads were taken from; without gains
+ * it is not read and may be NULL, like dgq and dgk. */
+fpsketch_status fpsketch_heads_grad(const void* dq, const void* dk, const void* dv, const float* C,
+                                    int64_t t, int32_t hq, int32_t hkv, int32_t hd, const float* gq,
+                                    const float* gk, double eps, const int64_t* pos,
+                                    const float* freq, int32_t rd, int32_t pairs,
+                                    fpsketch_dtype dtype, void* dC, float* dgq, float* dgk,
+                                    void* workspace, int64_t workspace_bytes, void* stream);
+int64_t fpsketch_heads_grad_workspace(int64_t t, int32_t hq, int32_t hkv, int32_t hd);
+
 #ifdef __cplusplus
 }
 #endif

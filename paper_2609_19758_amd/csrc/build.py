@@ -16,7 +16,7 @@ OUT = os.path.join(PKG, "libfpsketch.so")
 # (bench.py --wg-timeline reads it).  The binding never loads it for the probe path.
 OUT_TIMELINE = os.path.join(PKG, "libfpsketch_timeline.so")
 SOURCES = ["fpsk_stream.hip", "fpsk_wide.hip", "fpsk_kernels.hip", "fpsk_tables.hip", "fpsk_digits.hip",
-           "fpsk_host.hip"]
+           "fpsk_host.hip", "fpsk_gated.hip", "fpsk_adapters.hip", "fpsk_heads.hip"]
 
 # gfx950 only; packed FP32 instructions disabled (hipcc forms them from plain float code).
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

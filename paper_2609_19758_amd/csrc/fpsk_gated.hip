@@ -1,0 +1,592 @@
+// The gated feed-forward block around a delivered product (gfx950).
+//
+//   P = X W^T          X t x d, W 2f x d (f gate rows, then f up rows), FP32 sums
+//   H = act(G) U       G = P[:, :f], U = P[:, f:], rounded once to the half format
+//   dP = [dH U act'(G), dH act(G)]
+//   dX = dP W, dW = dP^T X
+//
+// All three products run in mm_kernel: a work-group takes a tile of the output over K in steps of
+// 64, both operands' tiles in LDS (two buffers), every wave a part of the tile in FP32
+// accumulators of the 16 x 16 x 32 matrix instruction.  An operand's tile is kept as it is stored:
+//   row-major (K contiguous)   rows of 64 k, read as 16-byte fragments;
+//   K-major (the product runs along the stored rows, W in dP W, both operands in dP^T X)
+//                              rows of one k, read with the transposing LDS read, which gives a
+//                              lane four k of one column: no operand is transposed in memory.
+#include "fpsk_layers.h"
+
+#include <algorithm>
+
+namespace fpsk {
+
+namespace {
+
+constexpr int kBK = 64;
+
+struct MmArgs {
+  const uint16_t* A;       // M x K, or K x M (K-major)
+  const uint16_t* B;       // N x K, or K x N (K-major)
+  int64_t M, N, K;
+  int64_t f;               // gated: N = 2f
+  float* out;              // M x N (gated: may be null)
+  uint16_t* H;             // gated: M x f
+  float* part;             // splits x M x N partial products, splits > 1
+  int64_t tiles_m, tiles_n;
+  int splits;
+  int64_t kslice;          // k per split, a multiple of kBK
+};
+
+// One operand's tile: R rows (row-major) or columns (K-major) by kBK, loaded by NT threads.
+//
+// In LDS, 16-byte groups are permuted within a row so that a wave's reads spread over the banks:
+// row-major group c of row r at c ^ ((r / 2) % 8) (the 16 rows of a fragment then cover all banks);
+// K-major the 32-byte pair s of row k at s ^ hash(k), which separates the 8 rows that half a wave
+// reads.
+//
+// GATE: tile rows are taken in blocks of 16, gate and up rows in turn, so that a wave holds both
+// halves of the same columns of H.
+template <int R, int NT, bool KM, bool GATE>
+struct Tile {
+  static constexpr int kLoads = R * 8 / NT;       // 16-byte groups per thread
+  static constexpr int kBytes = R * kBK * 2;
+  const uint16_t* X;
+  int64_t ld, lim, total;
+  int64_t off[kLoads];     // element offset of the group at k = 0; < 0: outside
+  int kk[kLoads];          // its k
+
+  static __device__ __forceinline__ int hash(int k) { return (k & 3) | ((k >> 1) & 4); }
+
+  __device__ void init(const uint16_t* x, int64_t r0, int64_t rows, int64_t ld_, int64_t f,
+                       int64_t total_) {
+    X = x;
+    ld = ld_;
+    lim = rows;
+    total = total_;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int L = i * NT + static_cast<int>(threadIdx.x);
+      if constexpr (KM) {
+        const int k = L / (R / 8), slot = L % (R / 8);
+        const int c = (((slot >> 1) ^ hash(k)) << 1) | (slot & 1);
+        const int64_t n = r0 + 8 * c;
+        kk[i] = k;
+        off[i] = n < rows ? static_cast<int64_t>(k) * ld + n : -1;
+      } else {
+        const int r = L >> 3, c = (L & 7) ^ ((r >> 1) & 7);
+        int64_t row = r0 + r;
+        bool ok = row < rows;
+        if constexpr (GATE) {
+          const int64_t j = r0 + ((r >> 5) << 4) + (r & 15);   // r0: the tile's first column of H
+          ok = j < f;
+          row = j + ((r >> 4) & 1) * f;
+        }
+        kk[i] = 8 * c;
+        off[i] = ok ? row * ld + 8 * c : -1;
+      }
+    }
+  }
+
+  // Group i at k0 .. k0 + kBK (< K), zero outside.
+  __device__ __forceinline__ u32x4 group(int i, int64_t k0, int64_t K) const {
+    const int64_t k = k0 + kk[i];
+    if constexpr (KM) {
+      const int64_t o = off[i] + k0 * ld;
+      const int64_t n = off[i] - static_cast<int64_t>(kk[i]) * ld;
+      return load_ragged(X, o, off[i] >= 0 && k < K ? lim - n : 0, total);
+    } else {
+      return load_ragged(X, off[i] + k0, off[i] >= 0 ? K - k : 0, total);
+    }
+  }
+
+  static __device__ __forceinline__ void put(char* lds, int i, u32x4 v) {
+    *reinterpret_cast<u32x4*>(lds + (i * NT + static_cast<int>(threadIdx.x)) * 16) = v;
+  }
+
+  // Fragment of rows (columns) n0 .. n0 + 15 and k = 32 ks .. 32 ks + 31.
+  static __device__ __forceinline__ u32x4 frag(const char* lds, int n0, int ks) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (KM) {
+      const int h = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
+      const int k = 32 * ks + 8 * (lane >> 4) + ((lane & 15) >> 2);
+      const char* p = lds + k * (2 * R) + (((n0 >> 4) ^ h) << 5) + 8 * (lane & 3);
+      typedef __attribute__((address_space(3))) s16x4* lp;
+      const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p)));
+      const u32x2 b = __builtin_bit_cast(
+          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * (2 * R))));
+      return u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+      const int r = n0 + (lane & 15), c = 4 * ks + (lane >> 4);
+      return *reinterpret_cast<const u32x4*>(lds + r * 128 + ((c ^ ((r >> 1) & 7)) << 4));
+    }
+  }
+};
+
+template <int ACT>
+__device__ __forceinline__ float gate_up(float g, float u) {
+  return g * act_gate<ACT>(g) * u;
+}
+
+template <int DT>
+__device__ __forceinline__ float gate_up(int act, float g, float u) {
+  return act == 0 ? gate_up<0>(g, u) : act == 1 ? gate_up<1>(g, u) : gate_up<2>(g, u);
+}
+
+// Four neighbours of a row of n, at column j.
+__device__ __forceinline__ void store4(float* row, int64_t j, int64_t n, f32x4 v, bool vec) {
+  if (vec && j + 3 < n) {
+    *reinterpret_cast<f32x4*>(row + j) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e < n) row[j + e] = v[e];
+    }
+  }
+}
+
+__device__ __forceinline__ void store4h(uint16_t* row, int64_t j, int64_t n, u16x4 v, bool vec) {
+  if (vec && j + 3 < n) {
+    *reinterpret_cast<u16x4*>(row + j) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e < n) row[j + e] = v[e];
+    }
+  }
+}
+
+// Work-groups are dealt to the 8 XCDs in turn; each XCD gets neighbouring tiles, in bands of 8 rows
+// of tiles, so that its L2 holds the operands' tiles that they share.
+__device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn, int64_t* m, int64_t* n) {
+  const int64_t count = tm * tn, per = count / 8;
+  if (b < 8 * per) b = (b % 8) * per + b / 8;
+  const int64_t band = b / (8 * tn), first = 8 * band;
+  const int64_t height = tm - first < 8 ? tm - first : 8;
+  const int64_t in = b - band * 8 * tn;
+  *m = first + in % height;
+  *n = in / height;
+}
+
+template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
+__global__ __launch_bounds__(64 * WM * WN) void mm_kernel(MmArgs a, int act) {
+  constexpr int NT = 64 * WM * WN;
+  constexpr int MT = BM / WM / 16, NTL = BN / WN / 16;
+  typedef Tile<BM, NT, AKM, false> TA;
+  typedef Tile<BN, NT, BKM, GATED> TB;
+  __shared__ __attribute__((aligned(16))) char lds_a[2][TA::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds_b[2][TB::kBytes];
+
+  const int64_t tiles = a.tiles_m * a.tiles_n;
+  const int64_t split = blockIdx.x / tiles;
+  int64_t tm, tn;
+  tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n, &tm, &tn);
+  const int64_t m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
+  const int64_t k0 = split * a.kslice;
+  const int64_t k1 = k0 + a.kslice < a.K ? k0 + a.kslice : a.K;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+
+  TA ta;
+  TB tb;
+  ta.init(a.A, m0, a.M, AKM ? a.M : a.K, 0, a.M * a.K);
+  tb.init(a.B, n0, a.N, BKM ? a.N : a.K, a.f, a.N * a.K);
+
+  f32x4 acc[MT][NTL];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  u32x4 ra[TA::kLoads], rb[TB::kLoads];
+  auto fetch = [&](int64_t k) {
+#pragma unroll
+    for (int i = 0; i < TA::kLoads; ++i) ra[i] = ta.group(i, k, k1);
+#pragma unroll
+    for (int i = 0; i < TB::kLoads; ++i) rb[i] = tb.group(i, k, k1);
+  };
+  auto keep = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < TA::kLoads; ++i) TA::put(lds_a[buf], i, ra[i]);
+#pragma unroll
+    for (int i = 0; i < TB::kLoads; ++i) TB::put(lds_b[buf], i, rb[i]);
+  };
+
+  int buf = 0;
+  if (k0 < k1) {
+    fetch(k0);
+    keep(0);
+  }
+  for (int64_t k = k0; k < k1; k += kBK) {
+    __syncthreads();
+    const bool more = k + kBK < k1;
+    if (more) fetch(k + kBK);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 fb[NTL];
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) fb[j] = TB::frag(lds_b[buf], wn + 16 * j, ks);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const u32x4 fa = TA::frag(lds_a[buf], wm + 16 * i, ks);
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[j], fa, acc[i][j]);
+      }
+    }
+    if (more) keep(buf ^ 1);
+    buf ^= 1;
+  }
+
+  // lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16 block
+  float* out = a.splits > 1 ? a.part + split * a.M * a.N : a.out;
+  const bool vec = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 &&
+                   (!GATED || (a.f & 3) == 0);
+  const bool vec_h = GATED && (a.f & 3) == 0 && (reinterpret_cast<uintptr_t>(a.H) & 7u) == 0;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + wm + 16 * i + (lane & 15);
+    if (m >= a.M) continue;
+    if constexpr (GATED) {
+#pragma unroll
+      for (int j = 0; j < NTL; j += 2) {
+        const int64_t n = n0 + ((wn + 16 * j) >> 1) + 4 * (lane >> 4);
+        const f32x4 g = acc[i][j], u = acc[i][j + 1];
+        if (out != nullptr) {
+          store4(out + m * a.N, n, a.f, g, vec);
+          store4(out + m * a.N + a.f, n, a.f, u, vec);
+        }
+        if (a.splits == 1) {
+          store4h(a.H + m * a.f, n, a.f,
+                  to_half4<DT>(gate_up<DT>(act, g[0], u[0]), gate_up<DT>(act, g[1], u[1]),
+                               gate_up<DT>(act, g[2], u[2]), gate_up<DT>(act, g[3], u[3])),
+                  vec_h);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) {
+        store4(out + m * a.N, n0 + wn + 16 * j + 4 * (lane >> 4), a.N, acc[i][j], vec);
+      }
+    }
+  }
+}
+
+// The sum of the partial products in the order of the splits: one element a thread (gated: one
+// element of H, two of P).
+template <int DT, bool GATED>
+__global__ __launch_bounds__(kThreads) void mm_sum_kernel(MmArgs a, int act) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
+  const int64_t count = a.M * (GATED ? a.f : a.N), size = a.M * a.N;
+  for (int64_t o = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; o < count; o += step) {
+    if constexpr (GATED) {
+      const int64_t m = o / a.f, at = m * a.N + (o - m * a.f);
+      float g = 0.0f, u = 0.0f;
+      for (int s = 0; s < a.splits; ++s) {
+        g += a.part[s * size + at];
+        u += a.part[s * size + at + a.f];
+      }
+      if (a.out != nullptr) {
+        a.out[at] = g;
+        a.out[at + a.f] = u;
+      }
+      a.H[o] = to_half<DT>(gate_up<DT>(act, g, u));
+    } else {
+      float v = 0.0f;
+      for (int s = 0; s < a.splits; ++s) v += a.part[s * size + o];
+      a.out[o] = v;
+    }
+  }
+}
+
+// H = act(G) U from a delivered product, one element a thread.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void narrow_kernel(const float* P, int64_t t, int64_t f,
+                                                          int act, uint16_t* H) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
+  for (int64_t o = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; o < t * f; o += step) {
+    const int64_t m = o / f, at = 2 * m * f + (o - m * f);
+    H[o] = to_half<DT>(gate_up<DT>(act, P[at], P[at + f]));
+  }
+}
+
+template <int ACT>
+__device__ __forceinline__ void grads(float g, float u, float dh, float* dg, float* du) {
+  const float s = act_gate<ACT>(g);
+  *dg = dh * u * act_slope<ACT>(g, s);
+  *du = dh * g * s;
+}
+
+// dP of a 32 x 32 block of H; the transpose goes through LDS so that its rows are written whole.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, const float* P,
+                                                        int64_t t, int64_t f, int act,
+                                                        uint16_t* dP, uint16_t* dPt,
+                                                        int64_t blocks_f) {
+  __shared__ uint16_t tile[2][32][33];
+  const int64_t m0 = (blockIdx.x / blocks_f) * 32, j0 = (blockIdx.x % blocks_f) * 32;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  for (int r = y; r < 32; r += 8) {
+    const int64_t m = m0 + r, j = j0 + x;
+    if (m < t && j < f) {
+      const int64_t at = 2 * m * f + j;
+      const float g = P[at], u = P[at + f], dh = from_half<DT>(dH[m * f + j]);
+      float dg, du;
+      if (act == 0) {
+        grads<0>(g, u, dh, &dg, &du);
+      } else if (act == 1) {
+        grads<1>(g, u, dh, &dg, &du);
+      } else {
+        grads<2>(g, u, dh, &dg, &du);
+      }
+      const uint16_t hg = to_half<DT>(dg), hu = to_half<DT>(du);
+      dP[at] = hg;
+      dP[at + f] = hu;
+      tile[0][r][x] = hg;
+      tile[1][r][x] = hu;
+    }
+  }
+  if (dPt == nullptr) return;
+  __syncthreads();
+  for (int r = y; r < 32; r += 8) {
+    const int64_t j = j0 + r, m = m0 + x;
+    if (m < t && j < f) {
+      dPt[j * t + m] = tile[0][x][r];
+      dPt[(j + f) * t + m] = tile[1][x][r];
+    }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+constexpr int kTile = 128;
+
+// How a product is cut: K is split while there are fewer tiles than would fill the chip twice over
+// and every split keeps at least 8 steps.
+struct Cut {
+  int64_t tiles_m, tiles_n, kslice;
+  int splits;
+};
+
+Cut cut_of(int64_t M, int64_t cols, int cols_per_tile, int64_t K, int cus) {
+  Cut c;
+  c.tiles_m = (M + kTile - 1) / kTile;
+  c.tiles_n = (cols + cols_per_tile - 1) / cols_per_tile;
+  const int64_t tiles = c.tiles_m * c.tiles_n, steps = (K + kBK - 1) / kBK;
+  int64_t s = 1;
+  if (tiles < 2 * cus) s = std::min<int64_t>(2 * cus / tiles, steps / 8);
+  s = std::max<int64_t>(1, s);
+  const int64_t per = std::max<int64_t>(1, (steps + s - 1) / s);
+  c.kslice = per * kBK;
+  c.splits = static_cast<int>(std::max<int64_t>(1, (steps + per - 1) / per));
+  return c;
+}
+
+template <int DT, bool AKM, bool BKM, bool GATED>
+hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
+  a.tiles_m = c.tiles_m;
+  a.tiles_n = c.tiles_n;
+  a.splits = c.splits;
+  a.kslice = c.kslice;
+  const auto grid = static_cast<unsigned>(c.tiles_m * c.tiles_n * c.splits);
+  FPSK_LAUNCH((mm_kernel<DT, kTile, kTile, 2, 2, AKM, BKM, GATED>), dim3(grid), dim3(256), 0, st, a,
+              act);
+  if (c.splits > 1) {
+    const int64_t count = a.M * (GATED ? a.f : a.N);
+    const auto g = static_cast<unsigned>(std::min<int64_t>((count + kThreads - 1) / kThreads, 8192));
+    FPSK_LAUNCH((mm_sum_kernel<DT, GATED>), dim3(g), dim3(kThreads), 0, st, a, act);
+  }
+  return hipSuccess;
+}
+
+bool dims_ok(int64_t t, int64_t d, int64_t f) {
+  if (t < 0 || d < 1 || f < 1 || t >= kDimLimit || d >= kDimLimit || f >= kDimLimit / 2) return false;
+  // element counts stay inside 2^40, and the tiles of a product inside one launch
+  const double most = 1099511627776.0;
+  const double td = static_cast<double>(t) * static_cast<double>(d);
+  const double tf = 2.0 * static_cast<double>(t) * static_cast<double>(f);
+  const double df = 2.0 * static_cast<double>(d) * static_cast<double>(f);
+  return td <= most && tf <= most && df <= most;
+}
+
+bool launch_fits(const Cut& c) {
+  return static_cast<double>(c.tiles_m) * c.tiles_n * c.splits * 512.0 < 4294967296.0;
+}
+
+int64_t part_bytes(const Cut& c, int64_t M, int64_t N) {
+  return c.splits > 1 ? static_cast<int64_t>(c.splits) * M * N * 4 : 0;
+}
+
+}  // namespace
+
+}  // namespace fpsk
+
+using namespace fpsk;
+
+extern "C" {
+
+int64_t fpsketch_gated_workspace(int64_t t, int64_t d, int64_t f) {
+  int cus = 0;
+  if (!dims_ok(t, d, f) || t == 0 || layer_device(&cus) != FPSK_OK) return 0;
+  return part_bytes(cut_of(t, f, kTile / 2, d, cus), t, 2 * f);
+}
+
+fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f,
+                               fpsketch_dtype dtype, fpsketch_act act, void* H, float* P,
+                               void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!half_type(dtype)) return layer_error(FPSK_EDTYPE, "fpsketch_gated: X, W and H are FP16 or BF16");
+  if (act < FPSK_SILU || act > FPSK_GELU_TANH) return layer_error(FPSK_EINVAL, "fpsketch_gated: unknown activation");
+  if (!dims_ok(t, d, f)) return layer_error(FPSK_ESHAPE, "fpsketch_gated: dimensions");
+  if (t == 0) return FPSK_OK;
+  if (X == nullptr || W == nullptr || H == nullptr) return layer_error(FPSK_EINVAL, "fpsketch_gated: null pointer");
+  if (!aligned(X, 2) || !aligned(W, 2) || !aligned(H, 2) || !aligned(P, 4)) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated: a pointer is not aligned to its elements");
+  }
+  int cus = 0;
+  const fpsketch_status s = layer_device(&cus);
+  if (s != FPSK_OK) return s;
+  const Cut c = cut_of(t, f, kTile / 2, d, cus);
+  const int64_t need = part_bytes(c, t, 2 * f);
+  if (!launch_fits(c)) return layer_error(FPSK_ESHAPE, "fpsketch_gated: too many tiles");
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16))) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated: workspace smaller than fpsketch_gated_workspace, or not aligned to 16 bytes");
+  }
+  const Span in[] = {{X, 2 * t * d}, {W, 4 * f * d}};
+  const Span out[] = {{H, 2 * t * f}, {P, 8 * t * f}, {workspace, need}};
+  if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated: an output overlaps another argument");
+  MmArgs a{};
+  a.A = static_cast<const uint16_t*>(X);
+  a.B = static_cast<const uint16_t*>(W);
+  a.M = t;
+  a.N = 2 * f;
+  a.K = d;
+  a.f = f;
+  a.out = P;
+  a.H = static_cast<uint16_t*>(H);
+  a.part = static_cast<float*>(workspace);
+  const auto st = static_cast<hipStream_t>(stream);
+  return launched(dtype == FPSK_BF16 ? launch_mm<1, false, false, true>(a, c, act, st)
+                                     : launch_mm<0, false, false, true>(a, c, act, st),
+                  "fpsketch_gated");
+}
+
+fpsketch_status fpsketch_gated_narrow(const float* P, int64_t t, int64_t f, fpsketch_dtype dtype,
+                                      fpsketch_act act, void* H, void* stream) {
+  if (!half_type(dtype)) return layer_error(FPSK_EDTYPE, "fpsketch_gated_narrow: H is FP16 or BF16");
+  if (act < FPSK_SILU || act > FPSK_GELU_TANH) return layer_error(FPSK_EINVAL, "fpsketch_gated_narrow: unknown activation");
+  if (!dims_ok(t, 1, f)) return layer_error(FPSK_ESHAPE, "fpsketch_gated_narrow: dimensions");
+  if (t == 0) return FPSK_OK;
+  if (P == nullptr || H == nullptr) return layer_error(FPSK_EINVAL, "fpsketch_gated_narrow: null pointer");
+  if (!aligned(P, 4) || !aligned(H, 2)) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated_narrow: a pointer is not aligned to its elements");
+  }
+  int cus = 0;
+  const fpsketch_status s = layer_device(&cus);
+  if (s != FPSK_OK) return s;
+  const Span in[] = {{P, 8 * t * f}};
+  const Span out[] = {{H, 2 * t * f}};
+  if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated_narrow: H overlaps P");
+  const auto st = static_cast<hipStream_t>(stream);
+  const auto grid = static_cast<unsigned>(std::min<int64_t>((t * f + kThreads - 1) / kThreads, 16384));
+  auto* h = static_cast<uint16_t*>(H);
+  return launched(dtype == FPSK_BF16
+                      ? launch_k(narrow_kernel<1>, dim3(grid), dim3(kThreads), 0, st, nullptr, nullptr,
+                                 P, t, f, static_cast<int>(act), h)
+                      : launch_k(narrow_kernel<0>, dim3(grid), dim3(kThreads), 0, st, nullptr, nullptr,
+                                 P, t, f, static_cast<int>(act), h),
+                  "fpsketch_gated_narrow");
+}
+
+fpsketch_status fpsketch_gated_grad(const void* dH, const float* P, int64_t t, int64_t f,
+                                    fpsketch_dtype dtype, fpsketch_act act, void* dP, void* dPt,
+                                    void* stream) {
+  if (!half_type(dtype)) return layer_error(FPSK_EDTYPE, "fpsketch_gated_grad: dH and dP are FP16 or BF16");
+  if (act < FPSK_SILU || act > FPSK_GELU_TANH) return layer_error(FPSK_EINVAL, "fpsketch_gated_grad: unknown activation");
+  if (!dims_ok(t, 1, f)) return layer_error(FPSK_ESHAPE, "fpsketch_gated_grad: dimensions");
+  if (t == 0) return FPSK_OK;
+  if (dH == nullptr || P == nullptr || dP == nullptr) return layer_error(FPSK_EINVAL, "fpsketch_gated_grad: null pointer");
+  if (!aligned(P, 4) || !aligned(dH, 2) || !aligned(dP, 2) || !aligned(dPt, 2)) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated_grad: a pointer is not aligned to its elements");
+  }
+  int cus = 0;
+  const fpsketch_status s = layer_device(&cus);
+  if (s != FPSK_OK) return s;
+  const Span in[] = {{dH, 2 * t * f}, {P, 8 * t * f}};
+  const Span out[] = {{dP, 4 * t * f}, {dPt, 4 * t * f}};
+  if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated_grad: an output overlaps another argument");
+  const int64_t bf = (f + 31) / 32, blocks = bf * ((t + 31) / 32);
+  if (blocks >= int64_t{1} << 24) return layer_error(FPSK_ESHAPE, "fpsketch_gated_grad: too many blocks");
+  const auto st = static_cast<hipStream_t>(stream);
+  const auto* dh = static_cast<const uint16_t*>(dH);
+  auto *o = static_cast<uint16_t*>(dP), *ot = static_cast<uint16_t*>(dPt);
+  const dim3 grid(static_cast<unsigned>(blocks));
+  return launched(dtype == FPSK_BF16
+                      ? launch_k(grad_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, dh, P, t,
+                                 f, static_cast<int>(act), o, ot, bf)
+                      : launch_k(grad_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, dh, P, t,
+                                 f, static_cast<int>(act), o, ot, bf),
+                  "fpsketch_gated_grad");
+}
+
+int64_t fpsketch_gated_products_workspace(int64_t t, int64_t d, int64_t f) {
+  int cus = 0;
+  if (!dims_ok(t, d, f) || layer_device(&cus) != FPSK_OK) return 0;
+  // the two products run one after the other and share it
+  const int64_t x = t > 0 ? part_bytes(cut_of(t, d, kTile, 2 * f, cus), t, d) : 0;
+  return std::max(x, part_bytes(cut_of(2 * f, d, kTile, t, cus), 2 * f, d));
+}
+
+fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const void* W, int64_t t,
+                                        int64_t d, int64_t f, fpsketch_dtype dtype, float* dX,
+                                        float* dW, void* workspace, int64_t workspace_bytes,
+                                        void* stream) {
+  if (!half_type(dtype)) return layer_error(FPSK_EDTYPE, "fpsketch_gated_products: dP, X and W are FP16 or BF16");
+  if (!dims_ok(t, d, f)) return layer_error(FPSK_ESHAPE, "fpsketch_gated_products: dimensions");
+  if (dX == nullptr && dW == nullptr) return layer_error(FPSK_EINVAL, "fpsketch_gated_products: no output");
+  if ((t > 0 && dP == nullptr) || (t > 0 && dW != nullptr && X == nullptr) ||
+      (t > 0 && dX != nullptr && W == nullptr)) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated_products: null pointer");
+  }
+  if (!aligned(dP, 2) || !aligned(X, 2) || !aligned(W, 2) || !aligned(dX, 4) || !aligned(dW, 4)) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated_products: a pointer is not aligned to its elements");
+  }
+  int cus = 0;
+  const fpsketch_status s = layer_device(&cus);
+  if (s != FPSK_OK) return s;
+  const Cut cx = cut_of(std::max<int64_t>(t, 1), d, kTile, 2 * f, cus);
+  const Cut cw = cut_of(2 * f, d, kTile, t, cus);
+  int64_t need = 0;
+  if (dX != nullptr && t > 0) need = part_bytes(cx, t, d);
+  if (dW != nullptr) need = std::max(need, part_bytes(cw, 2 * f, d));
+  if (!launch_fits(cx) || !launch_fits(cw)) return layer_error(FPSK_ESHAPE, "fpsketch_gated_products: too many tiles");
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16))) {
+    return layer_error(FPSK_EINVAL, "fpsketch_gated_products: workspace smaller than fpsketch_gated_products_workspace, or not aligned to 16 bytes");
+  }
+  const Span in[] = {{dP, 4 * t * f}, {X, 2 * t * d}, {W, 4 * f * d}};
+  const Span out[] = {{dX, 4 * t * d}, {dW, 8 * f * d}, {workspace, need}};
+  if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated_products: an output overlaps another argument");
+  const auto st = static_cast<hipStream_t>(stream);
+  hipError_t e = hipSuccess;
+  MmArgs a{};
+  a.part = static_cast<float*>(workspace);
+  if (dX != nullptr && t > 0) {
+    a.A = static_cast<const uint16_t*>(dP);
+    a.B = static_cast<const uint16_t*>(W);
+    a.M = t;
+    a.N = d;
+    a.K = 2 * f;
+    a.out = dX;
+    e = dtype == FPSK_BF16 ? launch_mm<1, false, true, false>(a, cx, 0, st)
+                           : launch_mm<0, false, true, false>(a, cx, 0, st);
+  }
+  if (e == hipSuccess && dW != nullptr) {
+    a.A = static_cast<const uint16_t*>(dP);
+    a.B = static_cast<const uint16_t*>(X);
+    a.M = 2 * f;
+    a.N = d;
+    a.K = t;
+    a.out = dW;
+    e = dtype == FPSK_BF16 ? launch_mm<1, true, true, false>(a, cw, 0, st)
+                           : launch_mm<0, true, true, false>(a, cw, 0, st);
+  }
+  return launched(e, "fpsketch_gated_products");
+}
+
+}  // extern "C"

@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -18,6 +19,7 @@
 
 #include "../../include/fpsketch.h"
 #include "fpsk_internal.h"
+#include "fpsk_layers.h"
 
 using fpsk::kColTile;
 using fpsk::kThreads;
@@ -1383,6 +1385,43 @@ int64_t window_coords(const WindowCheck& wc, const std::vector<int64_t>& centers
 
 // ==========================================================================================
 // C ABI.
+
+// ------------------------------------------------------------------------------------------
+// What the operators around a delivered product share with the verifier.
+
+namespace fpsk {
+
+fpsketch_status layer_error(fpsketch_status s, const char* detail) noexcept {
+  try {
+    g_last_error = detail;
+  } catch (...) {
+    g_last_error.clear();
+  }
+  return s;
+}
+
+fpsketch_status layer_device(int* cus) noexcept {
+  // the properties of a device are read once: the query takes longer than a small operator
+  constexpr int kMost = 64;
+  static std::atomic<int> known[kMost];          // 0: not read yet, -1: not gfx950, else its CUs
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess && dev >= 0 && dev < kMost && known[dev].load() != 0) {
+    *cus = known[dev].load();
+  } else if (e == hipSuccess) {
+    hipDeviceProp_t prop;
+    e = hipGetDeviceProperties(&prop, dev);
+    if (e == hipSuccess) {
+      const bool ours = std::strncmp(prop.gcnArchName, "gfx950", 6) == 0;
+      *cus = ours ? std::max(1, prop.multiProcessorCount) : -1;
+      if (dev >= 0 && dev < kMost) known[dev].store(*cus);
+    }
+  }
+  if (e != hipSuccess) return layer_error(FPSK_EHIP, hipGetErrorString(e));
+  return *cus > 0 ? FPSK_OK : layer_error(FPSK_ENODEV, "the current device is not gfx950");
+}
+
+}  // namespace fpsk
 
 extern "C" {
 

@@ -1,0 +1,164 @@
+// Shared by the operators around a delivered product (fpsk_gated.hip, fpsk_adapters.hip,
+// fpsk_heads.hip): vector types of the matrix instructions, rounding to the half formats, ragged
+// loads, activations, and the argument checks of their C entry points.
+#pragma once
+
+#include <cmath>
+#include <cstdint>
+#include <cstdio>
+
+#include "../../include/fpsketch.h"
+#include "fpsk_device.h"
+
+namespace fpsk {
+
+// fpsk_host.hip: keeps the detail of fpsketch_last_error and returns the status.
+fpsketch_status layer_error(fpsketch_status s, const char* detail) noexcept;
+
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// D += X Y on 16 x 16 x 32: lane l holds X[l % 16][8 (l / 16) + e] and Y[8 (l / 16) + e][l % 16],
+// e < 8, and D[4 (l / 16) + r][l % 16], r < 4.
+template <int DT>
+__device__ __forceinline__ f32x4 mfma32(u32x4 x, u32x4 y, f32x4 d) {
+  if constexpr (DT == 1) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
+                                                   __builtin_bit_cast(bf16x8, y), d, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x),
+                                                  __builtin_bit_cast(f16x8, y), d, 0, 0, 0);
+  }
+}
+
+// Round to nearest even.
+template <int DT>
+__device__ __forceinline__ uint16_t to_half(float x) {
+  if constexpr (DT == 1) {
+    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+  } else {
+    return __builtin_bit_cast(uint16_t, static_cast<_Float16>(x));
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ float from_half(uint16_t h) {
+  return lo_half<DT>(h);
+}
+
+template <int DT>
+__device__ __forceinline__ u16x4 to_half4(float a, float b, float c, float d) {
+  return u16x4{to_half<DT>(a), to_half<DT>(b), to_half<DT>(c), to_half<DT>(d)};
+}
+
+// Elements off .. off + 7 of an array of `total` half words, zero from the nv-th on (nv <= 0: all).
+// One 16-byte load at element alignment; near the end of the array the last whole group is loaded
+// and moved down, and an array of fewer than 8 elements is read one by one.
+__device__ __forceinline__ u32x4 load_ragged(const uint16_t* X, int64_t off, int64_t nv,
+                                             int64_t total) {
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (nv <= 0) return v;
+  const int n = nv < 8 ? static_cast<int>(nv) : 8;
+  if (off + 8 <= total) {
+    v = *reinterpret_cast<const u32x4_a2*>(X + off);
+  } else if (total >= 8) {
+    v = *reinterpret_cast<const u32x4_a2*>(X + total - 8);
+    const int s = static_cast<int>(off + 8 - total);
+    if (s & 1) {
+      v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16),
+                (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
+    }
+    if (s & 2) v = u32x4{v[1], v[2], v[3], 0u};
+    if (s & 4) v = u32x4{v[2], v[3], 0u, 0u};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (e < n) v[e / 2] |= static_cast<uint32_t>(X[off + e]) << (16 * (e & 1));
+    }
+  }
+  if (n < 8) v &= rag_keep(0, n);
+  return v;
+}
+
+// 1 / (1 + e^-x).  The hardware's exponential and reciprocal are within a few units of FP32's last
+// place, far below the half formats' half step that every result here is rounded by.
+__device__ __forceinline__ float sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+}
+
+// The activations act(x) of the gated block: 0 silu x s(x); 1 gelu x Phi(x), with Phi from erfc so
+// that the far negative side does not cancel; 2 its tanh form, 0.5 (1 + tanh y) = s(2 y).
+constexpr float kSqrtHalf = 0.70710678118654752f;
+constexpr float kGeluC = 1.5957691216057308f;     // 2 sqrt(2 / pi)
+constexpr float kGeluA = 0.044715f;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+
+template <int ACT>
+__device__ __forceinline__ float act_gate(float x) {   // act(x) = x act_gate(x)
+  if constexpr (ACT == 0) return sigmoid(x);
+  if constexpr (ACT == 1) return 0.5f * erfcf(-kSqrtHalf * x);
+  return sigmoid(kGeluC * (x + kGeluA * x * x * x));
+}
+
+// act'(x) given s = act_gate(x).  Where s has reached 0 or 1 the second term has vanished; it is
+// left out there because its factors overflow first.
+template <int ACT>
+__device__ __forceinline__ float act_slope(float x, float s) {
+  if constexpr (ACT == 0) return (s == 0.0f || s == 1.0f) ? s : s + x * s * (1.0f - s);
+  if constexpr (ACT == 1) {
+    const float e = x * x;
+    return e > 200.0f ? s : s + x * kInvSqrt2Pi * __expf(-0.5f * e);
+  }
+  return (s == 0.0f || s == 1.0f)
+             ? s
+             : s + x * s * (1.0f - s) * kGeluC * (1.0f + 3.0f * kGeluA * x * x);
+}
+
+// ---- host side of the entry points ---------------------------------------------------------
+
+constexpr int64_t kDimLimit = int64_t{1} << 31;
+
+struct Span {
+  const void* p;
+  int64_t bytes;
+};
+
+inline bool overlap(const Span& a, const Span& b) {
+  if (a.p == nullptr || b.p == nullptr || a.bytes <= 0 || b.bytes <= 0) return false;
+  const auto x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+}
+
+// Every output clear of every input and of the other outputs.
+template <int NI, int NO>
+bool disjoint(const Span (&in)[NI], const Span (&out)[NO]) {
+  for (int o = 0; o < NO; ++o) {
+    for (int i = 0; i < NI; ++i) {
+      if (overlap(out[o], in[i])) return false;
+    }
+    for (int p = 0; p < o; ++p) {
+      if (overlap(out[o], out[p])) return false;
+    }
+  }
+  return true;
+}
+
+inline bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+inline bool half_type(fpsketch_dtype t) { return t == FPSK_F16 || t == FPSK_BF16; }
+
+// Multiprocessors of the current device in *cus; FPSK_ENODEV unless it is a gfx950.
+fpsketch_status layer_device(int* cus) noexcept;
+
+// The status of an operator whose launches ended with e.
+inline fpsketch_status launched(hipError_t e, const char* where) noexcept {
+  if (e == hipSuccess) return FPSK_OK;
+  char msg[160];
+  std::snprintf(msg, sizeof(msg), "%s: %s", where, hipGetErrorString(e));
+  return layer_error(e == hipErrorOutOfMemory ? FPSK_ENOMEM : FPSK_EHIP, msg);
+}
+
+}  // namespace fpsk

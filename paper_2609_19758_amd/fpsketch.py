@@ -99,6 +99,24 @@ _SIGS = {
                                                  ctypes.POINTER(Params), ctypes.POINTER(_I32),
                                                  ctypes.POINTER(_I32)]),
     "fpsketch_rms_hat_samples": (_D, [ctypes.POINTER(ctypes.c_float), _I64]),
+    # operators around a delivered product (layers.py)
+    "fpsketch_gated": (ctypes.c_int, [_P, _P, _I64, _I64, _I64, ctypes.c_int, ctypes.c_int, _P, _P,
+                                      _P, _I64, _P]),
+    "fpsketch_gated_workspace": (_I64, [_I64, _I64, _I64]),
+    "fpsketch_gated_narrow": (ctypes.c_int, [_P, _I64, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
+    "fpsketch_gated_grad": (ctypes.c_int, [_P, _P, _I64, _I64, ctypes.c_int, ctypes.c_int, _P, _P,
+                                           _P]),
+    "fpsketch_gated_products": (ctypes.c_int, [_P, _P, _P, _I64, _I64, _I64, ctypes.c_int, _P, _P,
+                                               _P, _I64, _P]),
+    "fpsketch_gated_products_workspace": (_I64, [_I64, _I64, _I64]),
+    "fpsketch_adapters": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I32, _I32,
+                                         ctypes.c_int, _P, ctypes.c_int, _P, _I64, _P]),
+    "fpsketch_adapters_workspace": (_I64, [_I64, _I64, _I64, _I32, _I32]),
+    "fpsketch_heads": (ctypes.c_int, [_P, _I64, _I32, _I32, _I32, _P, _P, _D, _P, _P, _I32, _I32,
+                                      ctypes.c_int, _P, _P, _P, _P]),
+    "fpsketch_heads_grad": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I32, _I32, _I32, _P, _P, _D, _P,
+                                           _P, _I32, _I32, ctypes.c_int, _P, _P, _P, _P, _I64, _P]),
+    "fpsketch_heads_grad_workspace": (_I64, [_I64, _I32, _I32, _I32]),
 }
 
 _lib = None
