@@ -22,53 +22,416 @@ struct AdapterArgs {
   const float* scale;
   int64_t t, k, n;
   int count, rank;
-  float* V;                // t x rank: X_i A_a^T
+  float* V;                // splits x t x rank: partial sums of X_i A_a^T
   void* Y;
-  int half;                // Y in the half format
+  int64_t tiles;
+  int ways;                // work-groups that share a tile's adapters
+  int splits;              // parts of k
+  int blocks;              // rank blocks (shrink) or column blocks (expand)
 };
 
-// V, one row per wave.
-template <int DT>
-__global__ __launch_bounds__(kThreads) void shrink_kernel(AdapterArgs a) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + wave; i < a.t;
-       i += static_cast<int64_t>(gridDim.x) * 4) {
-    const int which = a.index[i];
-    if (which < 0 || which >= a.count) continue;
-    const uint16_t* x = a.X + i * a.k;
-    for (int j = 0; j < a.rank; ++j) {
-      const uint16_t* w = a.A + (static_cast<int64_t>(which) * a.rank + j) * a.k;
-      float s = 0.0f;
-      for (int64_t e = lane; e < a.k; e += 64) s += from_half<DT>(x[e]) * from_half<DT>(w[e]);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-      if (lane == 0) a.V[i * a.rank + j] = s;
-    }
+// Both kernels take tiles of neighbouring rows as they come, in two or three steps over the
+// adapters that a tile's rows name: an adapter's factor multiplies the whole tile on the matrix
+// cores, and only its own rows are kept.  The rows of a request are neighbours, so a prompt's tile
+// names one adapter or two and no sorting of rows is needed before; a decode tile names up to 16,
+// which `ways` work-groups take in turn.
+//
+// each(a, mask): a the adapter (-1: none, count: invalid), mask its rows in the tile.
+template <int TR, typename F>
+__device__ __forceinline__ void for_adapters(const AdapterArgs& a, int64_t row0, int way, F each) {
+  const int lane = threadIdx.x & 63;
+  const bool live = lane < TR && row0 + lane < a.t;
+  int which = live ? a.index[row0 + lane] : -1;
+  if (which < -1 || which > a.count) which = a.count;
+  uint64_t left = __ballot(live);
+  for (int c = 0; left != 0; ++c) {
+    const int b = __builtin_amdgcn_readlane(which, __builtin_ctzll(left));
+    const uint64_t mask = __ballot(live && which == b);
+    if (c % a.ways == way) each(b, mask);
+    left &= ~mask;
   }
 }
 
-// Y, one element a thread.
-template <int DT>
+// V = X A^T: a tile of 16 MT rows, a block of 16 NT ranks and a part of k per work-group.  Bound by
+// reading X once (the factors stay in L2); fragments come straight from memory, a wave's 64 k per
+// step as 32 bytes a lane, so that the four lanes of a row read a whole 128-byte line, with the next
+// step's loads in flight during the products.  The four waves take the steps in turn and their sums
+// meet in LDS; parts of k are added by the next kernel, in order.
+template <int DT, int MT, int NT>
+__global__ __launch_bounds__(kThreads) void shrink_kernel(AdapterArgs a) {
+  constexpr int TR = 16 * MT, RB = 16 * NT;
+  __shared__ __attribute__((aligned(16))) float red[4][TR][RB + 4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+  unsigned b = blockIdx.x;
+  const int split = b % a.splits;
+  b /= a.splits;
+  const int rb = b % a.blocks;
+  b /= a.blocks;
+  const int64_t row0 = static_cast<int64_t>(b % a.tiles) * TR;
+  const int way = static_cast<int>(b / a.tiles);   // last: most tiles name one adapter only
+  const int r0 = rb * RB;
+  const int64_t steps = a.k / 64;                  // whole ones
+
+  for_adapters<TR>(a, row0, way, [&](int which, uint64_t mask) {
+    if (which < 0 || which >= a.count) return;
+    // rows and ranks past the end repeat the last one; their sums are not stored
+    int64_t xo[MT], ao[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t r = row0 + 16 * i + (lane & 15);
+      xo[i] = (r < a.t ? r : a.t - 1) * a.k + 16 * g;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int r = r0 + 16 * j + (lane & 15);
+      ao[j] = (static_cast<int64_t>(which) * a.rank + (r < a.rank ? r : a.rank - 1)) * a.k + 16 * g;
+    }
+    const int64_t xall = a.t * a.k, aall = static_cast<int64_t>(a.count) * a.rank * a.k;
+    u32x4 x[MT][2], f[NT][2];
+    auto fetch = [&](int64_t s) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t k0 = 64 * s + 8 * h;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[i][h] = *reinterpret_cast<const u32x4_a2*>(a.X + xo[i] + k0);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) f[j][h] = *reinterpret_cast<const u32x4_a2*>(a.A + ao[j] + k0);
+      }
+    };
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int64_t stride = 4 * a.splits;
+    int64_t s = split * 4 + wave;
+    if (s < steps) fetch(s);
+    for (; s < steps; s += stride) {
+      u32x4 xc[MT][2], fc[NT][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xc[i][h] = x[i][h];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fc[j][h] = f[j][h];
+      }
+      if (s + stride < steps) fetch(s + stride);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma32<DT>(fc[j][h], xc[i][h], acc[i][j]);
+        }
+      }
+    }
+    if (s == steps && 64 * steps < a.k) {  // the wave whose turn the broken last step is
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t k0 = 64 * steps + 8 * h, nv = a.k - k0 - 16 * g;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[i][h] = load_ragged(a.X, xo[i] + k0, nv, xall);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const u32x4 w = load_ragged(a.A, ao[j] + k0, nv, aall);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) acc[i][j] = mfma32<DT>(w, x[i][h], acc[i][j]);
+        }
+      }
+    }
+    __syncthreads();                       // the sums of the adapter before
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        *reinterpret_cast<f32x4*>(&red[wave][16 * i + (lane & 15)][16 * j + 4 * g]) = acc[i][j];
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < TR * RB; e += kThreads) {
+      const int r = e / RB, c = e % RB;
+      if (((mask >> r) & 1) != 0 && r0 + c < a.rank) {
+        a.V[(static_cast<int64_t>(split) * a.t + row0 + r) * a.rank + r0 + c] =
+            (red[0][r][c] + red[1][r][c]) + (red[2][r][c] + red[3][r][c]);
+      }
+    }
+  });
+}
+
+// Y = C + s V B^T on a tile of 16 MT rows and 128 NC columns.  Bound by C and Y, whose loads and
+// stores are whole lines: the columns of a 32-wide block are dealt to two products so that a lane
+// holds 8 neighbours of one row.  V enters the matrix cores as two half words, hi + lo, so that
+// 16 (BF16) or 22 (FP16) of its bits count against the exact factor B; in FP16 a row is first
+// scaled by a power of two to where both words are in range.
+//
+// WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
+template <int DT, int MT, int NC, bool HALF, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
+  constexpr int TR = 16 * MT, PER = kThreads / TR;      // threads per row of V
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int rp = (a.rank + 31) / 32 * 32, ld = rp + 8;  // ranks as the products take them
+  uint16_t* hi = reinterpret_cast<uint16_t*>(smem);     // TR x ld
+  uint16_t* lo = hi + TR * ld;
+  float* sums = reinterpret_cast<float*>(lo + TR * ld); // TR x rp
+  float* back = sums + TR * rp;                         // TR: what undoes the scaling
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+  unsigned b = blockIdx.x;
+  const int64_t n0 = static_cast<int64_t>(b % a.blocks) * (128 * NC) + wave * (32 * NC);
+  b /= a.blocks;
+  const int64_t row0 = static_cast<int64_t>(b % a.tiles) * TR;
+  const int way = static_cast<int>(b / a.tiles);
+
+  for_adapters<TR>(a, row0, way, [&](int which, uint64_t mask) {
+    f32x4 y[MT][NC][2];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const bool own = ((mask >> (16 * i + (lane & 15))) & 1) != 0;
+      const float* c = a.C + (row0 + 16 * i + (lane & 15)) * a.n;
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        const int64_t col = n0 + 32 * q + 8 * g;
+        y[i][q][0] = y[i][q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (own && col + 8 <= a.n) {
+          y[i][q][0] = *reinterpret_cast<const f32x4_a4*>(c + col);
+          y[i][q][1] = *reinterpret_cast<const f32x4_a4*>(c + col + 4);
+        } else if (own) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (col + e < a.n) y[i][q][e / 4][e % 4] = c[col + e];
+          }
+        }
+      }
+    }
+    if (which >= 0 && which < a.count) {
+      __syncthreads();                     // the V of the adapter before
+      {
+        const int r = threadIdx.x / PER, p = threadIdx.x % PER;
+        const bool own = ((mask >> r) & 1) != 0;
+        const float* v = a.V + (row0 + r) * a.rank;
+        const int64_t part = a.t * a.rank;
+        float top = 0.0f;
+        for (int c = p; c < rp; c += PER) {
+          float s = 0.0f;
+          if (own && c < a.rank) {
+            for (int q = 0; q < a.splits; ++q) s += v[q * part + c];
+          }
+          sums[r * rp + c] = s;
+          top = fmaxf(top, fabsf(s));
+        }
+        float up = 1.0f, down = 1.0f;
+        if constexpr (DT == 0) {
+#pragma unroll
+          for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, PER));
+          if (top > 0.0f && top < __builtin_inff()) {
+            int e = ilogbf(top);
+            e = e < -126 ? -126 : (e > 126 ? 126 : e);
+            up = ldexpf(1.0f, -e);
+            down = ldexpf(1.0f, e);
+          }
+        }
+        for (int c = p; c < rp; c += PER) {
+          const float s = sums[r * rp + c] * up;
+          const uint16_t h = to_half<DT>(s);
+          const float rest = s - from_half<DT>(h);
+          hi[r * ld + c] = h;
+          lo[r * ld + c] = fabsf(s) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
+        }
+        if (p == 0) back[r] = down;
+      }
+      __syncthreads();
+      f32x4 acc[MT][NC][2];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int q = 0; q < NC; ++q) acc[i][q][0] = acc[i][q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+      const int64_t base = static_cast<int64_t>(which) * a.n, all = static_cast<int64_t>(a.count) * a.n * a.rank;
+      for (int s = 0; s < rp; s += 32) {
+        u32x4 f[NC][2];
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // row i of the product's 16 is column 8 (i / 4) + 4 h + i % 4 of the block
+            const int64_t col = n0 + 32 * q + 8 * ((lane & 15) >> 2) + 4 * h + (lane & 3);
+            const bool ok = col < a.n && s + 8 * g < a.rank;
+            const int64_t at = (base + col) * a.rank + s + 8 * g;
+            if constexpr (WHOLE) {
+              f[q][h] = *reinterpret_cast<const u32x4_a2*>(a.B + (ok ? at : 0));
+              if (!ok) f[q][h] = u32x4{0u, 0u, 0u, 0u};
+            } else {
+              f[q][h] = load_ragged(a.B, at, ok ? a.rank - s - 8 * g : 0, all);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int at = (16 * i + (lane & 15)) * ld + s + 8 * g;
+          const u32x4 vh = *reinterpret_cast<const u32x4*>(hi + at);
+          const u32x4 vl = *reinterpret_cast<const u32x4*>(lo + at);
+#pragma unroll
+          for (int q = 0; q < NC; ++q) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              acc[i][q][h] = mfma32<DT>(f[q][h], vl, acc[i][q][h]);
+              acc[i][q][h] = mfma32<DT>(f[q][h], vh, acc[i][q][h]);
+            }
+          }
+        }
+      }
+      const float scale = a.scale[which];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const float f = scale * back[16 * i + (lane & 15)];
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y[i][q][0][e] = fmaf(acc[i][q][0][e], f, y[i][q][0][e]);
+            y[i][q][1][e] = fmaf(acc[i][q][1][e], f, y[i][q][1][e]);
+          }
+        }
+      }
+    } else if (which >= 0) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[i][q][e / 4][e % 4] = __builtin_nanf("");
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      if (((mask >> (16 * i + (lane & 15))) & 1) == 0) continue;
+      const int64_t o = (row0 + 16 * i + (lane & 15)) * a.n;
+#pragma unroll
+      for (int q = 0; q < NC; ++q) {
+        const int64_t col = n0 + 32 * q + 8 * g;
+        const f32x4 u = y[i][q][0], v = y[i][q][1];
+        if constexpr (HALF) {
+          auto* w = static_cast<uint16_t*>(a.Y) + o;
+          const u16x4 p = to_half4<DT>(u[0], u[1], u[2], u[3]), r = to_half4<DT>(v[0], v[1], v[2], v[3]);
+          if (col + 8 <= a.n) {
+            const u32x2 pw = __builtin_bit_cast(u32x2, p), rw = __builtin_bit_cast(u32x2, r);
+            *reinterpret_cast<u32x4_a2*>(w + col) = u32x4{pw[0], pw[1], rw[0], rw[1]};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (col + e < a.n) w[col + e] = e < 4 ? p[e] : r[e - 4];
+            }
+          }
+        } else {
+          float* w = static_cast<float*>(a.Y) + o;
+          if (col + 8 <= a.n) {
+            *reinterpret_cast<f32x4_a4*>(w + col) = u;
+            *reinterpret_cast<f32x4_a4*>(w + col + 4) = v;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (col + e < a.n) w[col + e] = e < 4 ? u[e] : v[e - 4];
+            }
+          }
+        }
+      }
+    }
+  });
+}
+
+// Operands of fewer than 8 elements, which the 16-byte loads above do not fit: one output a thread.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void tiny_kernel(AdapterArgs a, int half) {
   const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
   for (int64_t o = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; o < a.t * a.n; o += step) {
     const int64_t i = o / a.n, j = o - i * a.n;
     const int which = a.index[i];
     float y = a.C[o];
     if (which >= 0 && which < a.count) {
-      const uint16_t* b = a.B + (static_cast<int64_t>(which) * a.n + j) * a.rank;
       float s = 0.0f;
-      for (int e = 0; e < a.rank; ++e) s += a.V[i * a.rank + e] * from_half<DT>(b[e]);
-      y += a.scale[which] * s;
+      for (int e = 0; e < a.rank; ++e) {
+        const int64_t f = static_cast<int64_t>(which) * a.rank + e;
+        float v = 0.0f;
+        for (int64_t c = 0; c < a.k; ++c) v = fmaf(from_half<DT>(a.X[i * a.k + c]), from_half<DT>(a.A[f * a.k + c]), v);
+        s = fmaf(v, from_half<DT>(a.B[(static_cast<int64_t>(which) * a.n + j) * a.rank + e]), s);
+      }
+      y = fmaf(a.scale[which], s, y);
     } else if (which != -1) {
       y = __builtin_nanf("");
     }
-    if (a.half) {
+    if (half) {
       static_cast<uint16_t*>(a.Y)[o] = to_half<DT>(y);
     } else {
       static_cast<float*>(a.Y)[o] = y;
     }
   }
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+// How the work is cut.  Long batches take 32 rows a tile (each factor is then read from L2 half as
+// often), short ones 16; k is split while the tiles leave compute units without a work-group and
+// every wave keeps two steps.
+struct Cut {
+  int mt;
+  int64_t tiles;
+  int ways, splits, nt, rank_blocks;
+};
+
+Cut cut_of(int64_t t, int64_t k, int count, int rank, int cus) {
+  Cut c;
+  c.mt = t > 1024 ? 2 : 1;
+  const int tr = 16 * c.mt;
+  c.tiles = (t + tr - 1) / tr;
+  c.nt = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
+  c.rank_blocks = (rank + 16 * c.nt - 1) / (16 * c.nt);
+  const int64_t most = std::min<int64_t>(tr, int64_t{count} + 2);
+  c.ways = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 1024 / c.tiles)));
+  const int64_t steps = (k + 63) / 64;
+  const int64_t groups = c.tiles * c.rank_blocks;
+  c.splits = static_cast<int>(std::max<int64_t>(
+      1, std::min<int64_t>({int64_t{2} * cus / groups, steps / 8, int64_t{16}})));
+  return c;
+}
+
+template <int DT, int MT>
+hipError_t launch_shrink(const AdapterArgs& a, int nt, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks * a.splits)), block(kThreads);
+  if (nt == 1) FPSK_LAUNCH((shrink_kernel<DT, MT, 1>), grid, block, 0, st, a);
+  if (nt == 2) FPSK_LAUNCH((shrink_kernel<DT, MT, 2>), grid, block, 0, st, a);
+  if (nt == 4) FPSK_LAUNCH((shrink_kernel<DT, MT, 4>), grid, block, 0, st, a);
+  if (nt == 8) FPSK_LAUNCH((shrink_kernel<DT, MT, 8>), grid, block, 0, st, a);
+  return hipSuccess;
+}
+
+template <int DT, int MT, bool HALF, bool WHOLE>
+hipError_t launch_expand(AdapterArgs a, hipStream_t st) {
+  constexpr int NC = MT;
+  const auto kernel = expand_kernel<DT, MT, NC, HALF, WHOLE>;
+  a.blocks = static_cast<int>((a.n + 128 * NC - 1) / (128 * NC));
+  const int rp = (a.rank + 31) / 32 * 32;
+  const size_t lds = static_cast<size_t>(16 * MT) * (4 * (rp + 8) + 4 * rp + 4);
+  const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks)), block(kThreads);
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+    if (e != hipSuccess) return e;
+  }
+  FPSK_LAUNCH(kernel, grid, block, lds, st, a);
+  return hipSuccess;
+}
+
+template <int DT, int MT>
+hipError_t launch_adapters(AdapterArgs a, const Cut& c, bool half, hipStream_t st) {
+  a.tiles = c.tiles;
+  a.ways = c.ways;
+  a.splits = c.splits;
+  a.blocks = c.rank_blocks;
+  const hipError_t e = launch_shrink<DT, MT>(a, c.nt, st);
+  if (e != hipSuccess) return e;
+  if (a.rank % 8 == 0) return half ? launch_expand<DT, MT, true, true>(a, st) : launch_expand<DT, MT, false, true>(a, st);
+  return half ? launch_expand<DT, MT, true, false>(a, st) : launch_expand<DT, MT, false, false>(a, st);
 }
 
 bool adapter_dims(int64_t t, int64_t k, int64_t n, int32_t count, int32_t rank) {
@@ -88,7 +451,9 @@ using namespace fpsk;
 extern "C" {
 
 int64_t fpsketch_adapters_workspace(int64_t t, int64_t k, int64_t n, int32_t count, int32_t rank) {
-  return adapter_dims(t, k, n, count, rank) ? 4 * t * rank : 0;
+  int cus = 0;
+  if (!adapter_dims(t, k, n, count, rank) || t == 0 || layer_device(&cus) != FPSK_OK) return 0;
+  return 4 * t * rank * cut_of(t, k, count, rank, cus).splits;
 }
 
 fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, const void* B,
@@ -111,7 +476,13 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
   int cus = 0;
   const fpsketch_status s = layer_device(&cus);
   if (s != FPSK_OK) return s;
-  const int64_t need = fpsketch_adapters_workspace(t, k, n, count, rank);
+  const Cut c = cut_of(t, k, count, rank, cus);
+  const int64_t need = 4 * t * rank * c.splits;
+  // work-groups of the two launches: 128 columns or 16 ranks at least, a compute unit's worth of
+  // ways and parts of k at most
+  if (static_cast<double>(c.tiles) * c.ways * std::max<double>((n + 127) / 128, c.rank_blocks * c.splits) * kThreads >= 4294967296.0) {
+    return layer_error(FPSK_ESHAPE, "fpsketch_adapters: too many tiles");
+  }
   if (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16)) {
     return layer_error(FPSK_EINVAL, "fpsketch_adapters: workspace smaller than fpsketch_adapters_workspace, or not aligned to 16 bytes");
   }
@@ -133,17 +504,16 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
   a.rank = rank;
   a.V = static_cast<float*>(workspace);
   a.Y = Y;
-  a.half = half;
   const auto st = static_cast<hipStream_t>(stream);
-  const dim3 g1(static_cast<unsigned>(std::min<int64_t>((t + 3) / 4, 65536)));
-  const dim3 g2(static_cast<unsigned>(std::min<int64_t>((t * n + kThreads - 1) / kThreads, 16384)));
-  hipError_t e = dtype == FPSK_BF16
-                     ? launch_k(shrink_kernel<1>, g1, dim3(kThreads), 0, st, nullptr, nullptr, a)
-                     : launch_k(shrink_kernel<0>, g1, dim3(kThreads), 0, st, nullptr, nullptr, a);
-  if (e == hipSuccess) {
-    e = dtype == FPSK_BF16
-            ? launch_k(expand_kernel<1>, g2, dim3(kThreads), 0, st, nullptr, nullptr, a)
-            : launch_k(expand_kernel<0>, g2, dim3(kThreads), 0, st, nullptr, nullptr, a);
+  hipError_t e;
+  if (t * k < 8 || k * rank * count < 8 || n * rank * count < 8) {
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>((t * n + kThreads - 1) / kThreads, 4096)));
+    e = dtype == FPSK_BF16 ? launch_k(tiny_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half})
+                           : launch_k(tiny_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half});
+  } else if (dtype == FPSK_BF16) {
+    e = c.mt == 2 ? launch_adapters<1, 2>(a, c, half, st) : launch_adapters<1, 1>(a, c, half, st);
+  } else {
+    e = c.mt == 2 ? launch_adapters<0, 2>(a, c, half, st) : launch_adapters<0, 1>(a, c, half, st);
   }
   return launched(e, "fpsketch_adapters");
 }

@@ -269,6 +269,26 @@ __global__ __launch_bounds__(64 * WM * WN) void mm_kernel(MmArgs a, int act) {
   }
 }
 
+// A product with an operand of fewer than 8 elements, which 16-byte loads do not fit: one output
+// (gated: one of H) a thread.  sa, sb: strides of A and B along k, ra, rb along their rows.
+template <int DT, bool GATED>
+__global__ __launch_bounds__(kThreads) void tiny_kernel(MmArgs a, int64_t ra, int64_t sa, int64_t rb,
+                                                        int64_t sb, int act) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
+  const int64_t cols = GATED ? a.f : a.N;
+  for (int64_t o = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; o < a.M * cols; o += step) {
+    const int64_t m = o / cols, n = o - m * cols;
+    float v[2] = {0.0f, 0.0f};
+    for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+      for (int64_t k = 0; k < a.K; ++k) {
+        v[h] = fmaf(from_half<DT>(a.A[m * ra + k * sa]), from_half<DT>(a.B[(n + h * a.f) * rb + k * sb]), v[h]);
+      }
+      if (a.out != nullptr) a.out[m * a.N + n + h * a.f] = v[h];
+    }
+    if constexpr (GATED) a.H[o] = to_half<DT>(gate_up<DT>(act, v[0], v[1]));
+  }
+}
+
 // The sum of the partial products in the order of the splits: one element a thread (gated: one
 // element of H, two of P).
 template <int DT, bool GATED>
@@ -381,6 +401,13 @@ Cut cut_of(int64_t M, int64_t cols, int cols_per_tile, int64_t K, int cus) {
 
 template <int DT, bool AKM, bool BKM, bool GATED>
 hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
+  if (a.K > 0 && (a.M * a.K < 8 || a.N * a.K < 8)) {
+    const int64_t count = a.M * (GATED ? a.f : a.N);
+    const auto g = static_cast<unsigned>(std::min<int64_t>((count + kThreads - 1) / kThreads, 8192));
+    FPSK_LAUNCH((tiny_kernel<DT, GATED>), dim3(g), dim3(kThreads), 0, st, a, AKM ? 1 : a.K,
+                AKM ? a.M : 1, BKM ? 1 : a.K, BKM ? a.N : 1, act);
+    return hipSuccess;
+  }
   a.tiles_m = c.tiles_m;
   a.tiles_n = c.tiles_n;
   a.splits = c.splits;

@@ -54,33 +54,21 @@ __device__ __forceinline__ u16x4 to_half4(float a, float b, float c, float d) {
   return u16x4{to_half<DT>(a), to_half<DT>(b), to_half<DT>(c), to_half<DT>(d)};
 }
 
-// Elements off .. off + 7 of an array of `total` half words, zero from the nv-th on (nv <= 0: all).
-// One 16-byte load at element alignment; near the end of the array the last whole group is loaded
-// and moved down, and an array of fewer than 8 elements is read one by one.
+// Elements off .. off + 7 of an array of total >= 8 half words, zero from the nv-th on (nv <= 0:
+// all; off may then lie outside).  One 16-byte load at element alignment without a branch: near the
+// end of the array the last whole group is loaded and moved down.
 __device__ __forceinline__ u32x4 load_ragged(const uint16_t* X, int64_t off, int64_t nv,
                                              int64_t total) {
-  u32x4 v = {0u, 0u, 0u, 0u};
-  if (nv <= 0) return v;
-  const int n = nv < 8 ? static_cast<int>(nv) : 8;
-  if (off + 8 <= total) {
-    v = *reinterpret_cast<const u32x4_a2*>(X + off);
-  } else if (total >= 8) {
-    v = *reinterpret_cast<const u32x4_a2*>(X + total - 8);
-    const int s = static_cast<int>(off + 8 - total);
-    if (s & 1) {
-      v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16),
-                (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
-    }
-    if (s & 2) v = u32x4{v[1], v[2], v[3], 0u};
-    if (s & 4) v = u32x4{v[2], v[3], 0u, 0u};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (e < n) v[e / 2] |= static_cast<uint32_t>(X[off + e]) << (16 * (e & 1));
-    }
+  const int64_t last = total - 8, o = off < 0 || nv <= 0 ? 0 : (off < last ? off : last);
+  u32x4 v = *reinterpret_cast<const u32x4_a2*>(X + o);
+  const int s = nv <= 0 ? 0 : static_cast<int>(off - o);
+  if (s & 1) {
+    v = u32x4{(v[0] >> 16) | (v[1] << 16), (v[1] >> 16) | (v[2] << 16),
+              (v[2] >> 16) | (v[3] << 16), v[3] >> 16};
   }
-  if (n < 8) v &= rag_keep(0, n);
-  return v;
+  if (s & 2) v = u32x4{v[1], v[2], v[3], 0u};
+  if (s & 4) v = u32x4{v[2], v[3], 0u, 0u};
+  return v & rag_keep(0, nv);
 }
 
 // 1 / (1 + e^-x).  The hardware's exponential and reciprocal are within a few units of FP32's last
