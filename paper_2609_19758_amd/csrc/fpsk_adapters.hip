@@ -8,6 +8,7 @@
 #include "fpsk_layers.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fpsk {
 
@@ -28,6 +29,7 @@ struct AdapterArgs {
   int ways;                // work-groups that share a tile's adapters
   int splits;              // parts of k
   int blocks;              // rank blocks (shrink) or column blocks (expand)
+  int64_t cols;            // columns per column block
 };
 
 // Both kernels take tiles of neighbouring rows as they come, in two or three steps over the
@@ -52,15 +54,18 @@ __device__ __forceinline__ void for_adapters(const AdapterArgs& a, int64_t row0,
   }
 }
 
+constexpr int kShrinkWaves = 4;
+constexpr int kMaxSplits = 8;
+
 // V = X A^T: a tile of 16 MT rows, a block of 16 NT ranks and a part of k per work-group.  Bound by
 // reading X once (the factors stay in L2); fragments come straight from memory, a wave's 64 k per
 // step as 32 bytes a lane, so that the four lanes of a row read a whole 128-byte line, with the next
-// step's loads in flight during the products.  The four waves take the steps in turn and their sums
+// step's loads in flight during the products.  The waves take the steps in turn and their sums
 // meet in LDS; parts of k are added by the next kernel, in order.
 template <int DT, int MT, int NT>
-__global__ __launch_bounds__(kThreads) void shrink_kernel(AdapterArgs a) {
+__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, RB = 16 * NT;
-  __shared__ __attribute__((aligned(16))) float red[4][TR][RB + 4];
+  __shared__ __attribute__((aligned(16))) float red[kShrinkWaves][TR][RB + 4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
   unsigned b = blockIdx.x;
   const int split = b % a.splits;
@@ -87,16 +92,17 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AdapterArgs a) {
       ao[j] = (static_cast<int64_t>(which) * a.rank + (r < a.rank ? r : a.rank - 1)) * a.k + 16 * g;
     }
     const int64_t xall = a.t * a.k, aall = static_cast<int64_t>(a.count) * a.rank * a.k;
-    u32x4 x[MT][2], f[NT][2];
-    auto fetch = [&](int64_t s) {
+    u32x4 x[2][MT][2], f[2][NT][2];
+    auto fetch = [&](int b, int64_t s) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t k0 = 64 * s + 8 * h;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) x[i][h] = *reinterpret_cast<const u32x4_a2*>(a.X + xo[i] + k0);
+        for (int i = 0; i < MT; ++i) x[b][i][h] = *reinterpret_cast<const u32x4_a2*>(a.X + xo[i] + k0);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) f[j][h] = *reinterpret_cast<const u32x4_a2*>(a.A + ao[j] + k0);
+        for (int j = 0; j < NT; ++j) f[b][j][h] = *reinterpret_cast<const u32x4_a2*>(a.A + ao[j] + k0);
       }
+      __builtin_amdgcn_sched_barrier(0);   // (else the loads sink to where they are used)
     };
     f32x4 acc[MT][NT];
 #pragma unroll
@@ -104,39 +110,45 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AdapterArgs a) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    const int64_t stride = 4 * a.splits;
-    int64_t s = split * 4 + wave;
-    if (s < steps) fetch(s);
-    for (; s < steps; s += stride) {
-      u32x4 xc[MT][2], fc[NT][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) xc[i][h] = x[i][h];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) fc[j][h] = f[j][h];
-      }
-      if (s + stride < steps) fetch(s + stride);
+    auto multiply = [&](int b) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = mfma32<DT>(fc[j][h], xc[i][h], acc[i][j]);
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma32<DT>(f[b][j][h], x[b][i][h], acc[i][j]);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // Unconditional loads: behind a branch the compiler waits for the step ahead too.  A wave past
+    // its last step reads that one again.
+    const int64_t stride = kShrinkWaves * a.splits;
+    const int64_t first = split * kShrinkWaves + __builtin_amdgcn_readfirstlane(wave);
+    const int64_t mine = first < steps ? (steps - first - 1) / stride + 1 : 0;
+    if (mine > 0) {
+      const int64_t end = first + (mine - 1) * stride;
+      fetch(0, first);
+      int64_t s = first;
+      for (int64_t left = mine; left > 1; left -= 2, s += 2 * stride) {
+        fetch(1, s + stride);
+        multiply(0);
+        fetch(0, s + 2 * stride < end ? s + 2 * stride : end);
+        multiply(1);
+      }
+      if (mine & 1) multiply(0);
     }
-    if (s == steps && 64 * steps < a.k) {  // the wave whose turn the broken last step is
+    if (first + mine * stride == steps && 64 * steps < a.k) {  // the wave whose turn the broken last step is
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t k0 = 64 * steps + 8 * h, nv = a.k - k0 - 16 * g;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) x[i][h] = load_ragged(a.X, xo[i] + k0, nv, xall);
+        for (int i = 0; i < MT; ++i) x[0][i][h] = load_ragged(a.X, xo[i] + k0, nv, xall);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           const u32x4 w = load_ragged(a.A, ao[j] + k0, nv, aall);
 #pragma unroll
-          for (int i = 0; i < MT; ++i) acc[i][j] = mfma32<DT>(w, x[i][h], acc[i][j]);
+          for (int i = 0; i < MT; ++i) acc[i][j] = mfma32<DT>(w, x[0][i][h], acc[i][j]);
         }
       }
     }
@@ -149,21 +161,23 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AdapterArgs a) {
       }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < TR * RB; e += kThreads) {
+    for (int e = threadIdx.x; e < TR * RB; e += 64 * kShrinkWaves) {
       const int r = e / RB, c = e % RB;
       if (((mask >> r) & 1) != 0 && r0 + c < a.rank) {
-        a.V[(static_cast<int64_t>(split) * a.t + row0 + r) * a.rank + r0 + c] =
-            (red[0][r][c] + red[1][r][c]) + (red[2][r][c] + red[3][r][c]);
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kShrinkWaves; ++w) v += red[w][r][c];
+        a.V[(static_cast<int64_t>(split) * a.t + row0 + r) * a.rank + r0 + c] = v;
       }
     }
   });
 }
 
-// Y = C + s V B^T on a tile of 16 MT rows and 128 NC columns.  Bound by C and Y, whose loads and
-// stores are whole lines: the columns of a 32-wide block are dealt to two products so that a lane
-// holds 8 neighbours of one row.  V enters the matrix cores as two half words, hi + lo, so that
-// 16 (BF16) or 22 (FP16) of its bits count against the exact factor B; in FP16 a row is first
-// scaled by a power of two to where both words are in range.
+// Y = C + s V B^T on a tile of 16 MT rows and `cols` columns, 128 NC of them at a time.  Bound by C
+// and Y, whose loads and stores are whole lines: the columns of a 32-wide block are dealt to two
+// products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as two half
+// words, hi + lo, so that 16 (BF16) or 22 (FP16) of its bits count against the exact factor B; in
+// FP16 a row is first scaled by a power of two to where both words are in range.
 //
 // WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
 template <int DT, int MT, int NC, bool HALF, bool WHOLE>
@@ -175,87 +189,76 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
   uint16_t* lo = hi + TR * ld;
   float* sums = reinterpret_cast<float*>(lo + TR * ld); // TR x rp
   float* back = sums + TR * rp;                         // TR: what undoes the scaling
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   unsigned b = blockIdx.x;
-  const int64_t n0 = static_cast<int64_t>(b % a.blocks) * (128 * NC) + wave * (32 * NC);
+  const int64_t c0 = static_cast<int64_t>(b % a.blocks) * a.cols;
   b /= a.blocks;
   const int64_t row0 = static_cast<int64_t>(b % a.tiles) * TR;
   const int way = static_cast<int>(b / a.tiles);
+  const int64_t c1 = c0 + a.cols < a.n ? c0 + a.cols : a.n;
 
   for_adapters<TR>(a, row0, way, [&](int which, uint64_t mask) {
-    f32x4 y[MT][NC][2];
+    const bool mine = which >= 0 && which < a.count;
+    const int64_t base = static_cast<int64_t>(which) * a.n, all = static_cast<int64_t>(a.count) * a.n * a.rank;
+    float scale[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const bool own = ((mask >> (16 * i + (lane & 15))) & 1) != 0;
-      const float* c = a.C + (row0 + 16 * i + (lane & 15)) * a.n;
-#pragma unroll
-      for (int q = 0; q < NC; ++q) {
-        const int64_t col = n0 + 32 * q + 8 * g;
-        y[i][q][0] = y[i][q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (own && col + 8 <= a.n) {
-          y[i][q][0] = *reinterpret_cast<const f32x4_a4*>(c + col);
-          y[i][q][1] = *reinterpret_cast<const f32x4_a4*>(c + col + 4);
-        } else if (own) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (col + e < a.n) y[i][q][e / 4][e % 4] = c[col + e];
-          }
-        }
-      }
-    }
-    if (which >= 0 && which < a.count) {
+    for (int i = 0; i < MT; ++i) scale[i] = 0.0f;
+    if (mine) {
       __syncthreads();                     // the V of the adapter before
-      {
-        const int r = threadIdx.x / PER, p = threadIdx.x % PER;
-        const bool own = ((mask >> r) & 1) != 0;
-        const float* v = a.V + (row0 + r) * a.rank;
-        const int64_t part = a.t * a.rank;
-        float top = 0.0f;
-        for (int c = p; c < rp; c += PER) {
-          float s = 0.0f;
-          if (own && c < a.rank) {
-            for (int q = 0; q < a.splits; ++q) s += v[q * part + c];
-          }
-          sums[r * rp + c] = s;
-          top = fmaxf(top, fabsf(s));
-        }
-        float up = 1.0f, down = 1.0f;
-        if constexpr (DT == 0) {
+      const int r = threadIdx.x / PER, p = threadIdx.x % PER;
+      const bool own = ((mask >> r) & 1) != 0;
+      const float* v = a.V + (own ? row0 + r : row0) * a.rank;
+      const int64_t part = a.t * a.rank;
+      float top = 0.0f;
+      for (int c = p; c < rp; c += PER) {
+        float s = 0.0f;
+        if (own && c < a.rank) {
+          float w[kMaxSplits];             // all loads in flight, then the sum in order
 #pragma unroll
-          for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, PER));
-          if (top > 0.0f && top < __builtin_inff()) {
-            int e = ilogbf(top);
-            e = e < -126 ? -126 : (e > 126 ? 126 : e);
-            up = ldexpf(1.0f, -e);
-            down = ldexpf(1.0f, e);
-          }
+          for (int q = 0; q < kMaxSplits; ++q) w[q] = v[(q < a.splits ? q * part : 0) + c];
+#pragma unroll
+          for (int q = 0; q < kMaxSplits; ++q) s += q < a.splits ? w[q] : 0.0f;
         }
-        for (int c = p; c < rp; c += PER) {
-          const float s = sums[r * rp + c] * up;
-          const uint16_t h = to_half<DT>(s);
-          const float rest = s - from_half<DT>(h);
-          hi[r * ld + c] = h;
-          lo[r * ld + c] = fabsf(s) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
-        }
-        if (p == 0) back[r] = down;
+        sums[r * rp + c] = s;
+        top = fmaxf(top, fabsf(s));
       }
+      float up = 1.0f, down = 1.0f;
+      if constexpr (DT == 0) {
+#pragma unroll
+        for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, PER));
+        if (top > 0.0f && top < __builtin_inff()) {
+          int e = ilogbf(top);
+          e = e < -126 ? -126 : (e > 126 ? 126 : e);
+          up = ldexpf(1.0f, -e);
+          down = ldexpf(1.0f, e);
+        }
+      }
+      for (int c = p; c < rp; c += PER) {
+        const float s = sums[r * rp + c] * up;
+        const uint16_t h = to_half<DT>(s);
+        const float rest = s - from_half<DT>(h);
+        hi[r * ld + c] = h;
+        lo[r * ld + c] = fabsf(s) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
+      }
+      if (p == 0) back[r] = down;
       __syncthreads();
-      f32x4 acc[MT][NC][2];
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-#pragma unroll
-        for (int q = 0; q < NC; ++q) acc[i][q][0] = acc[i][q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-      const int64_t base = static_cast<int64_t>(which) * a.n, all = static_cast<int64_t>(a.count) * a.n * a.rank;
-      for (int s = 0; s < rp; s += 32) {
-        u32x4 f[NC][2];
+      for (int i = 0; i < MT; ++i) scale[i] = a.scale[which] * back[16 * i + (lane & 15)];
+    }
+
+    // FULL: the wave's columns all lie in the row; C is then loaded without a branch (rows of other
+    // adapters too: they are not stored here).
+    auto columns = [&](int64_t n0, auto full) {
+      constexpr bool FULL = decltype(full)::value;
+      u32x4 f[NC][2];
+      auto fetch = [&](int s) {
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             // row i of the product's 16 is column 8 (i / 4) + 4 h + i % 4 of the block
             const int64_t col = n0 + 32 * q + 8 * ((lane & 15) >> 2) + 4 * h + (lane & 3);
-            const bool ok = col < a.n && s + 8 * g < a.rank;
+            const bool ok = (FULL || col < a.n) && s + 8 * g < a.rank;
             const int64_t at = (base + col) * a.rank + s + 8 * g;
             if constexpr (WHOLE) {
               f[q][h] = *reinterpret_cast<const u32x4_a2*>(a.B + (ok ? at : 0));
@@ -265,76 +268,110 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
             }
           }
         }
+      };
+      if (mine) fetch(0);
+      f32x4 y[MT][NC][2];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int64_t r = row0 + 16 * i + (lane & 15);
+        const float* c = a.C + (r < a.t ? r : a.t - 1) * a.n;
+#pragma unroll
+        for (int q = 0; q < NC; ++q) {
+          const int64_t col = n0 + 32 * q + 8 * g;
+          if constexpr (FULL) {
+            y[i][q][0] = *reinterpret_cast<const f32x4_a4*>(c + col);
+            y[i][q][1] = *reinterpret_cast<const f32x4_a4*>(c + col + 4);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[i][q][e / 4][e % 4] = col + e < a.n ? c[col + e] : 0.0f;
+          }
+        }
+      }
+      if (mine) {
+        f32x4 acc[MT][NC][2];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const int at = (16 * i + (lane & 15)) * ld + s + 8 * g;
-          const u32x4 vh = *reinterpret_cast<const u32x4*>(hi + at);
-          const u32x4 vl = *reinterpret_cast<const u32x4*>(lo + at);
+#pragma unroll
+          for (int q = 0; q < NC; ++q) acc[i][q][0] = acc[i][q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        for (int s = 0; s < rp; s += 32) {
+          if (s > 0) fetch(s);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            const int at = (16 * i + (lane & 15)) * ld + s + 8 * g;
+            const u32x4 vh = *reinterpret_cast<const u32x4*>(hi + at);
+            const u32x4 vl = *reinterpret_cast<const u32x4*>(lo + at);
+#pragma unroll
+            for (int q = 0; q < NC; ++q) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                acc[i][q][h] = mfma32<DT>(f[q][h], vl, acc[i][q][h]);
+                acc[i][q][h] = mfma32<DT>(f[q][h], vh, acc[i][q][h]);
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
 #pragma unroll
           for (int q = 0; q < NC; ++q) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              acc[i][q][h] = mfma32<DT>(f[q][h], vl, acc[i][q][h]);
-              acc[i][q][h] = mfma32<DT>(f[q][h], vh, acc[i][q][h]);
+            for (int e = 0; e < 4; ++e) {
+              y[i][q][0][e] = fmaf(acc[i][q][0][e], scale[i], y[i][q][0][e]);
+              y[i][q][1][e] = fmaf(acc[i][q][1][e], scale[i], y[i][q][1][e]);
             }
           }
         }
+      } else if (which >= 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+          for (int q = 0; q < NC; ++q) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[i][q][e / 4][e % 4] = __builtin_nanf("");
+          }
+        }
       }
-      const float scale = a.scale[which];
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        const float f = scale * back[16 * i + (lane & 15)];
+        if (((mask >> (16 * i + (lane & 15))) & 1) == 0) continue;
+        const int64_t o = (row0 + 16 * i + (lane & 15)) * a.n;
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
+          const int64_t col = n0 + 32 * q + 8 * g;
+          const f32x4 u = y[i][q][0], v = y[i][q][1];
+          if constexpr (HALF) {
+            auto* w = static_cast<uint16_t*>(a.Y) + o;
+            const u16x4 p = to_half4<DT>(u[0], u[1], u[2], u[3]), r = to_half4<DT>(v[0], v[1], v[2], v[3]);
+            if (FULL) {
+              const u32x2 pw = __builtin_bit_cast(u32x2, p), rw = __builtin_bit_cast(u32x2, r);
+              *reinterpret_cast<u32x4_a2*>(w + col) = u32x4{pw[0], pw[1], rw[0], rw[1]};
+            } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[i][q][0][e] = fmaf(acc[i][q][0][e], f, y[i][q][0][e]);
-            y[i][q][1][e] = fmaf(acc[i][q][1][e], f, y[i][q][1][e]);
-          }
-        }
-      }
-    } else if (which >= 0) {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-#pragma unroll
-        for (int q = 0; q < NC; ++q) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[i][q][e / 4][e % 4] = __builtin_nanf("");
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if (((mask >> (16 * i + (lane & 15))) & 1) == 0) continue;
-      const int64_t o = (row0 + 16 * i + (lane & 15)) * a.n;
-#pragma unroll
-      for (int q = 0; q < NC; ++q) {
-        const int64_t col = n0 + 32 * q + 8 * g;
-        const f32x4 u = y[i][q][0], v = y[i][q][1];
-        if constexpr (HALF) {
-          auto* w = static_cast<uint16_t*>(a.Y) + o;
-          const u16x4 p = to_half4<DT>(u[0], u[1], u[2], u[3]), r = to_half4<DT>(v[0], v[1], v[2], v[3]);
-          if (col + 8 <= a.n) {
-            const u32x2 pw = __builtin_bit_cast(u32x2, p), rw = __builtin_bit_cast(u32x2, r);
-            *reinterpret_cast<u32x4_a2*>(w + col) = u32x4{pw[0], pw[1], rw[0], rw[1]};
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (col + e < a.n) w[col + e] = e < 4 ? p[e] : r[e - 4];
+              for (int e = 0; e < 8; ++e) {
+                if (col + e < a.n) w[col + e] = e < 4 ? p[e] : r[e - 4];
+              }
             }
-          }
-        } else {
-          float* w = static_cast<float*>(a.Y) + o;
-          if (col + 8 <= a.n) {
-            *reinterpret_cast<f32x4_a4*>(w + col) = u;
-            *reinterpret_cast<f32x4_a4*>(w + col + 4) = v;
           } else {
+            float* w = static_cast<float*>(a.Y) + o;
+            if (FULL) {
+              *reinterpret_cast<f32x4_a4*>(w + col) = u;
+              *reinterpret_cast<f32x4_a4*>(w + col + 4) = v;
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (col + e < a.n) w[col + e] = e < 4 ? u[e] : v[e - 4];
+              for (int e = 0; e < 8; ++e) {
+                if (col + e < a.n) w[col + e] = e < 4 ? u[e] : v[e - 4];
+              }
             }
           }
         }
+      }
+    };
+    for (int64_t n0 = c0 + wave * (32 * NC); n0 < c1; n0 += 128 * NC) {
+      if (n0 + 32 * NC <= a.n) {
+        columns(n0, std::true_type{});
+      } else {
+        columns(n0, std::false_type{});
       }
     }
   });
@@ -371,8 +408,9 @@ __global__ __launch_bounds__(kThreads) void tiny_kernel(AdapterArgs a, int half)
 // ---- host ------------------------------------------------------------------------------------
 
 // How the work is cut.  Long batches take 32 rows a tile (each factor is then read from L2 half as
-// often), short ones 16; k is split while the tiles leave compute units without a work-group and
-// every wave keeps two steps.
+// often), short ones 16.  k is split in up to 8 parts, part p on XCD p (work-groups are dealt to the
+// XCDs in turn), so that an XCD's L2 holds its part of the factors for all tiles; not where the
+// partial sums would be more than half of X, unless compute units would have no work-group.
 struct Cut {
   int mt;
   int64_t tiles;
@@ -387,17 +425,17 @@ Cut cut_of(int64_t t, int64_t k, int count, int rank, int cus) {
   c.nt = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
   c.rank_blocks = (rank + 16 * c.nt - 1) / (16 * c.nt);
   const int64_t most = std::min<int64_t>(tr, int64_t{count} + 2);
-  c.ways = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 1024 / c.tiles)));
-  const int64_t steps = (k + 63) / 64;
-  const int64_t groups = c.tiles * c.rank_blocks;
-  c.splits = static_cast<int>(std::max<int64_t>(
-      1, std::min<int64_t>({int64_t{2} * cus / groups, steps / 8, int64_t{16}})));
+  c.ways = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 256 / c.tiles)));
+  const int64_t steps = (k + 63) / 64, groups = c.tiles * c.rank_blocks;
+  const int64_t worth = std::max<int64_t>(k / (8 * int64_t{rank}), cus / groups);
+  c.splits = static_cast<int>(
+      std::max<int64_t>(1, std::min<int64_t>({worth, steps / kShrinkWaves, int64_t{kMaxSplits}})));
   return c;
 }
 
 template <int DT, int MT>
 hipError_t launch_shrink(const AdapterArgs& a, int nt, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks * a.splits)), block(kThreads);
+  const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks * a.splits)), block(64 * kShrinkWaves);
   if (nt == 1) FPSK_LAUNCH((shrink_kernel<DT, MT, 1>), grid, block, 0, st, a);
   if (nt == 2) FPSK_LAUNCH((shrink_kernel<DT, MT, 2>), grid, block, 0, st, a);
   if (nt == 4) FPSK_LAUNCH((shrink_kernel<DT, MT, 4>), grid, block, 0, st, a);
@@ -406,10 +444,15 @@ hipError_t launch_shrink(const AdapterArgs& a, int nt, hipStream_t st) {
 }
 
 template <int DT, int MT, bool HALF, bool WHOLE>
-hipError_t launch_expand(AdapterArgs a, hipStream_t st) {
+hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
   constexpr int NC = MT;
   const auto kernel = expand_kernel<DT, MT, NC, HALF, WHOLE>;
-  a.blocks = static_cast<int>((a.n + 128 * NC - 1) / (128 * NC));
+  // a work-group forms the tile's V once for all its columns: as many as leave three work-groups for
+  // every compute unit
+  const int64_t steps = (a.n + 128 * NC - 1) / (128 * NC);
+  const int64_t each = std::max<int64_t>(1, std::min<int64_t>(steps, a.tiles * steps / (3 * cus)));
+  a.cols = each * 128 * NC;
+  a.blocks = static_cast<int>((a.n + a.cols - 1) / a.cols);
   const int rp = (a.rank + 31) / 32 * 32;
   const size_t lds = static_cast<size_t>(16 * MT) * (4 * (rp + 8) + 4 * rp + 4);
   const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks)), block(kThreads);
@@ -423,15 +466,15 @@ hipError_t launch_expand(AdapterArgs a, hipStream_t st) {
 }
 
 template <int DT, int MT>
-hipError_t launch_adapters(AdapterArgs a, const Cut& c, bool half, hipStream_t st) {
+hipError_t launch_adapters(AdapterArgs a, const Cut& c, bool half, int cus, hipStream_t st) {
   a.tiles = c.tiles;
   a.ways = c.ways;
   a.splits = c.splits;
   a.blocks = c.rank_blocks;
   const hipError_t e = launch_shrink<DT, MT>(a, c.nt, st);
   if (e != hipSuccess) return e;
-  if (a.rank % 8 == 0) return half ? launch_expand<DT, MT, true, true>(a, st) : launch_expand<DT, MT, false, true>(a, st);
-  return half ? launch_expand<DT, MT, true, false>(a, st) : launch_expand<DT, MT, false, false>(a, st);
+  if (a.rank % 8 == 0) return half ? launch_expand<DT, MT, true, true>(a, cus, st) : launch_expand<DT, MT, false, true>(a, cus, st);
+  return half ? launch_expand<DT, MT, true, false>(a, cus, st) : launch_expand<DT, MT, false, false>(a, cus, st);
 }
 
 bool adapter_dims(int64_t t, int64_t k, int64_t n, int32_t count, int32_t rank) {
@@ -511,9 +554,9 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
     e = dtype == FPSK_BF16 ? launch_k(tiny_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half})
                            : launch_k(tiny_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half});
   } else if (dtype == FPSK_BF16) {
-    e = c.mt == 2 ? launch_adapters<1, 2>(a, c, half, st) : launch_adapters<1, 1>(a, c, half, st);
+    e = c.mt == 2 ? launch_adapters<1, 2>(a, c, half, cus, st) : launch_adapters<1, 1>(a, c, half, cus, st);
   } else {
-    e = c.mt == 2 ? launch_adapters<0, 2>(a, c, half, st) : launch_adapters<0, 1>(a, c, half, st);
+    e = c.mt == 2 ? launch_adapters<0, 2>(a, c, half, cus, st) : launch_adapters<0, 1>(a, c, half, cus, st);
   }
   return launched(e, "fpsketch_adapters");
 }
