@@ -27,7 +27,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # and the 64 x 64 product tile took 192 registers (2 waves per SIMD) instead of 98.  The digit
 # product's 224 accumulators belong in the AGPRs: in VGPRs they left 30 copies a step.
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-NO_VGPR_FORM = {"fpsk_digits.hip"}
+NO_VGPR_FORM = {"fpsk_digits.hip", "fpsk_gated.hip"}
 
 
 def hipcc() -> str:

@@ -120,6 +120,65 @@ struct Tile {
   }
 };
 
+// The same tile filled by loads that go straight to LDS: 16-byte groups on 16-byte boundaries (rows a
+// multiple of 8 long), 32-bit offsets within the tile (ld at most kMaxLd).  A wave's 64 groups land in
+// order, so the permutation is in the addresses.  Rows past the end repeat the last one, whose
+// products are not stored; k past K reads zeros.
+constexpr int64_t kMaxLd = int64_t{1} << 22;
+
+__device__ const u32x4 kZeros[4] = {};
+
+template <int R, int NT, bool KM, bool GATE>
+struct Direct {
+  static constexpr int kLoads = R * 8 / NT;
+  static constexpr int kRows = 8 * NT / R;   // K-major: k rows per load
+  static_assert(NT % 128 == 0 && (KM ? kRows : NT / 8) % 16 == 0, "the permutation is the same for every load");
+  const char* base;        // the wave's tile at k = 0
+  int64_t step;            // bytes from one k to the next
+  uint32_t at[KM ? 1 : kLoads];
+  uint32_t rows_on;        // K-major: bytes from one load's rows to the next's
+  int kk;                  // k of the first group (K-major: kRows on with each load)
+
+  __device__ void init(const uint16_t* x, int64_t r0, int64_t rows, int64_t ld, int64_t f) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), L = threadIdx.x;
+    // gate or up rows: 16 tile rows each in turn, 8 to a wave
+    const int64_t first = GATE ? r0 + ((wave >> 1) & 1) * f : r0;
+    base = reinterpret_cast<const char*>(x + (KM ? r0 : first * ld));
+    step = KM ? 2 * ld : 2;
+    rows_on = static_cast<uint32_t>(2 * kRows * ld);
+    if constexpr (KM) {
+      kk = L / (R / 8);
+      const int slot = L % (R / 8);
+      const int c = (((slot >> 1) ^ Tile<R, NT, KM, GATE>::hash(kk)) << 1) | (slot & 1);
+      at[0] = static_cast<uint32_t>(2 * (kk * ld + (r0 + 8 * c < rows ? 8 * c : rows - 8 - r0)));
+    } else {
+      const int c = (L & 7) ^ ((L >> 4) & 7);
+      kk = 8 * c;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = (i * NT + L) >> 3;
+        const int64_t j = GATE ? ((r >> 5) << 4) + (r & 15) : r, lim = GATE ? f : rows;
+        at[i] = static_cast<uint32_t>(2 * ((r0 + j < lim ? j : lim - 1 - r0) * ld + 8 * c));
+      }
+    }
+  }
+
+  // The tile at k0; TAIL: zeros from K on.
+  template <bool TAIL>
+  __device__ __forceinline__ void load(char* lds, int64_t k0, int64_t K) const {
+    const char* from = base + k0 * step;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const char* p = from + (KM ? i * static_cast<int64_t>(rows_on) : 0) + at[KM ? 0 : i];
+      if (TAIL && k0 + kk + (KM ? i * kRows : 0) >= K) p = reinterpret_cast<const char*>(kZeros);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p),
+                                       (__attribute__((address_space(3))) void*)(lds + (i * NT + 64 * wave) * 16),
+                                       16, 0, 0);
+    }
+  }
+};
+
 template <int ACT>
 __device__ __forceinline__ float gate_up(float g, float u) {
   return g * act_gate<ACT>(g) * u;
@@ -165,43 +224,119 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn, int64
   *n = in / height;
 }
 
+// Accumulators of a wave: BM / WM x BN / WN of the tile.
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
-__global__ __launch_bounds__(64 * WM * WN) void mm_kernel(MmArgs a, int act) {
-  constexpr int NT = 64 * WM * WN;
-  constexpr int MT = BM / WM / 16, NTL = BN / WN / 16;
+struct Wave {
+  static constexpr int NT = 64 * WM * WN;
+  static constexpr int MT = BM / WM / 16, NTL = BN / WN / 16;
   typedef Tile<BM, NT, AKM, false> TA;
   typedef Tile<BN, NT, BKM, GATED> TB;
-  __shared__ __attribute__((aligned(16))) char lds_a[2][TA::kBytes];
-  __shared__ __attribute__((aligned(16))) char lds_b[2][TB::kBytes];
-
-  const int64_t tiles = a.tiles_m * a.tiles_n;
-  const int64_t split = blockIdx.x / tiles;
-  int64_t tm, tn;
-  tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n, &tm, &tn);
-  const int64_t m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
-  const int64_t k0 = split * a.kslice;
-  const int64_t k1 = k0 + a.kslice < a.K ? k0 + a.kslice : a.K;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
-
-  TA ta;
-  TB tb;
-  ta.init(a.A, m0, a.M, AKM ? a.M : a.K, 0, a.M * a.K);
-  tb.init(a.B, n0, a.N, BKM ? a.N : a.K, a.f, a.N * a.K);
-
   f32x4 acc[MT][NTL];
+  int wm, wn;
+
+  __device__ void init() {
+    const int wave = threadIdx.x >> 6;
+    wm = (wave / WN) * (BM / WM);
+    wn = (wave % WN) * (BN / WN);
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
+    for (int i = 0; i < MT; ++i) {
 #pragma unroll
-    for (int j = 0; j < NTL; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j = 0; j < NTL; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
   }
 
+  __device__ __forceinline__ void multiply(const char* la, const char* lb) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 fb[NTL];
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) fb[j] = TB::frag(lb, wn + 16 * j, ks);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const u32x4 fa = TA::frag(la, wm + 16 * i, ks);
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[j], fa, acc[i][j]);
+      }
+    }
+  }
+
+  // lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16 block
+  __device__ void store(const MmArgs& a, int64_t m0, int64_t n0, int64_t split, int act) const {
+    const int lane = threadIdx.x & 63;
+    float* out = a.splits > 1 ? a.part + split * a.M * a.N : a.out;
+    const bool vec = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 &&
+                     (!GATED || (a.f & 3) == 0);
+    const bool vec_h = GATED && (a.f & 3) == 0 && (reinterpret_cast<uintptr_t>(a.H) & 7u) == 0;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t m = m0 + wm + 16 * i + (lane & 15);
+      if (m >= a.M) continue;
+      if constexpr (GATED) {
+#pragma unroll
+        for (int j = 0; j < NTL; j += 2) {
+          const int64_t n = n0 + ((wn + 16 * j) >> 1) + 4 * (lane >> 4);
+          const f32x4 g = acc[i][j], u = acc[i][j + 1];
+          if (out != nullptr) {
+            store4(out + m * a.N, n, a.f, g, vec);
+            store4(out + m * a.N + a.f, n, a.f, u, vec);
+          }
+          if (a.splits == 1) {
+            store4h(a.H + m * a.f, n, a.f,
+                    to_half4<DT>(gate_up<DT>(act, g[0], u[0]), gate_up<DT>(act, g[1], u[1]),
+                                 gate_up<DT>(act, g[2], u[2]), gate_up<DT>(act, g[3], u[3])),
+                    vec_h);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) {
+          store4(out + m * a.N, n0 + wn + 16 * j + 4 * (lane >> 4), a.N, acc[i][j], vec);
+        }
+      }
+    }
+  }
+};
+
+// A work-group's part of the product.
+struct Part {
+  int64_t m0, n0, k0, k1, split;
+};
+
+template <int BM, int BN, bool GATED>
+__device__ __forceinline__ Part part_of(const MmArgs& a) {
+  const int64_t tiles = a.tiles_m * a.tiles_n;
+  Part p;
+  int64_t tm, tn;
+  p.split = blockIdx.x / tiles;
+  tile_of(blockIdx.x - p.split * tiles, a.tiles_m, a.tiles_n, &tm, &tn);
+  p.m0 = tm * BM;
+  p.n0 = tn * (GATED ? BN / 2 : BN);
+  p.k0 = p.split * a.kslice;
+  p.k1 = p.k0 + a.kslice < a.K ? p.k0 + a.kslice : a.K;
+  return p;
+}
+
+// Any alignment: the operands' tiles pass through registers.
+template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mm_ragged_kernel(MmArgs a, int act) {
+  typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
+  typedef typename W::TA TA;
+  typedef typename W::TB TB;
+  __shared__ __attribute__((aligned(16))) char lds_a[2][TA::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds_b[2][TB::kBytes];
+  const Part p = part_of<BM, BN, GATED>(a);
+  TA ta;
+  TB tb;
+  ta.init(a.A, p.m0, a.M, AKM ? a.M : a.K, 0, a.M * a.K);
+  tb.init(a.B, p.n0, a.N, BKM ? a.N : a.K, a.f, a.N * a.K);
+  W w;
+  w.init();
   u32x4 ra[TA::kLoads], rb[TB::kLoads];
   auto fetch = [&](int64_t k) {
 #pragma unroll
-    for (int i = 0; i < TA::kLoads; ++i) ra[i] = ta.group(i, k, k1);
+    for (int i = 0; i < TA::kLoads; ++i) ra[i] = ta.group(i, k, p.k1);
 #pragma unroll
-    for (int i = 0; i < TB::kLoads; ++i) rb[i] = tb.group(i, k, k1);
+    for (int i = 0; i < TB::kLoads; ++i) rb[i] = tb.group(i, k, p.k1);
   };
   auto keep = [&](int buf) {
 #pragma unroll
@@ -209,64 +344,76 @@ __global__ __launch_bounds__(64 * WM * WN) void mm_kernel(MmArgs a, int act) {
 #pragma unroll
     for (int i = 0; i < TB::kLoads; ++i) TB::put(lds_b[buf], i, rb[i]);
   };
-
   int buf = 0;
-  if (k0 < k1) {
-    fetch(k0);
+  if (p.k0 < p.k1) {
+    fetch(p.k0);
     keep(0);
   }
-  for (int64_t k = k0; k < k1; k += kBK) {
+  for (int64_t k = p.k0; k < p.k1; k += kBK) {
     __syncthreads();
-    const bool more = k + kBK < k1;
+    const bool more = k + kBK < p.k1;
     if (more) fetch(k + kBK);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      u32x4 fb[NTL];
-#pragma unroll
-      for (int j = 0; j < NTL; ++j) fb[j] = TB::frag(lds_b[buf], wn + 16 * j, ks);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const u32x4 fa = TA::frag(lds_a[buf], wm + 16 * i, ks);
-#pragma unroll
-        for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[j], fa, acc[i][j]);
-      }
-    }
+    w.multiply(lds_a[buf], lds_b[buf]);
     if (more) keep(buf ^ 1);
     buf ^= 1;
   }
+  w.store(a, p.m0, p.n0, p.split, act);
+}
 
-  // lane l: row l % 16, columns 4 (l / 16) .. + 3 of every 16 x 16 block
-  float* out = a.splits > 1 ? a.part + split * a.M * a.N : a.out;
-  const bool vec = (a.N & 3) == 0 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 &&
-                   (!GATED || (a.f & 3) == 0);
-  const bool vec_h = GATED && (a.f & 3) == 0 && (reinterpret_cast<uintptr_t>(a.H) & 7u) == 0;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t m = m0 + wm + 16 * i + (lane & 15);
-    if (m >= a.M) continue;
-    if constexpr (GATED) {
-#pragma unroll
-      for (int j = 0; j < NTL; j += 2) {
-        const int64_t n = n0 + ((wn + 16 * j) >> 1) + 4 * (lane >> 4);
-        const f32x4 g = acc[i][j], u = acc[i][j + 1];
-        if (out != nullptr) {
-          store4(out + m * a.N, n, a.f, g, vec);
-          store4(out + m * a.N + a.f, n, a.f, u, vec);
-        }
-        if (a.splits == 1) {
-          store4h(a.H + m * a.f, n, a.f,
-                  to_half4<DT>(gate_up<DT>(act, g[0], u[0]), gate_up<DT>(act, g[1], u[1]),
-                               gate_up<DT>(act, g[2], u[2]), gate_up<DT>(act, g[3], u[3])),
-                  vec_h);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NTL; ++j) {
-        store4(out + m * a.N, n0 + wn + 16 * j + 4 * (lane >> 4), a.N, acc[i][j], vec);
-      }
+// Waits for this wave's loads to LDS, then for the work-group: afterwards every wave's are there, and
+// every wave has done with the buffer that the next loads go to.
+__device__ __forceinline__ void loads_done() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// Whole 16-byte groups: the next step's tiles go straight to LDS during the products of this one.
+template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) {
+  typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
+  // one array a buffer, so that the compiler knows loads into one apart from reads of the other
+  __shared__ __attribute__((aligned(16))) char a0[W::TA::kBytes];
+  __shared__ __attribute__((aligned(16))) char b0[W::TB::kBytes];
+  __shared__ __attribute__((aligned(16))) char a1[W::TA::kBytes];
+  __shared__ __attribute__((aligned(16))) char b1[W::TB::kBytes];
+  const Part p = part_of<BM, BN, GATED>(a);
+  Direct<BM, W::NT, AKM, false> da;
+  Direct<BN, W::NT, BKM, GATED> db;
+  da.init(a.A, p.m0, a.M, AKM ? a.M : a.K, 0);
+  db.init(a.B, p.n0, a.N, BKM ? a.N : a.K, a.f);
+  W w;
+  w.init();
+  auto load = [&](char* la, char* lb, int64_t k) {
+    da.template load<false>(la, k, p.k1);
+    db.template load<false>(lb, k, p.k1);
+    __builtin_amdgcn_sched_barrier(0);     // (else the loads sink to the end of the products)
+  };
+  // Whole steps; the last one is loaded again where no other follows.
+  int64_t n = (p.k1 - p.k0) / kBK, k = p.k0;
+  const int64_t last = p.k0 + (n - 1) * kBK;
+  if (n > 0) {
+    load(a0, b0, k);
+    for (; n > 1; n -= 2, k += 2 * kBK) {
+      loads_done();
+      load(a1, b1, k + kBK);
+      w.multiply(a0, b0);
+      loads_done();
+      load(a0, b0, k + 2 * kBK < last ? k + 2 * kBK : last);
+      w.multiply(a1, b1);
+    }
+    loads_done();                          // also where nothing is left: no load outlives the kernel
+    if (n == 1) {
+      w.multiply(a0, b0);
+      k += kBK;
     }
   }
+  if (k < p.k1) {                          // the broken step (every wave has left a1 and b1)
+    da.template load<true>(a1, k, p.k1);
+    db.template load<true>(b1, k, p.k1);
+    loads_done();
+    w.multiply(a1, b1);
+  }
+  w.store(a, p.m0, p.n0, p.split, act);
 }
 
 // A product with an operand of fewer than 8 elements, which 16-byte loads do not fit: one output
@@ -376,27 +523,38 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, cons
 
 // ---- host ------------------------------------------------------------------------------------
 
-constexpr int kTile = 128;
-
-// How a product is cut: K is split while there are fewer tiles than would fill the chip twice over
-// and every split keeps at least 8 steps.
+// How a product is cut: tiles of 256 x 256 where they fill the chip, else of 128 x 128, with K in
+// parts while those would not fill it twice over and every part keeps at least 8 steps.
 struct Cut {
+  bool big, direct;
   int64_t tiles_m, tiles_n, kslice;
   int splits;
 };
 
-Cut cut_of(int64_t M, int64_t cols, int cols_per_tile, int64_t K, int cus) {
+// cols: columns of the product, or of H (two of the product each).
+Cut cut_of(int64_t M, int64_t cols, bool gated, int64_t K, bool direct, int cus) {
   Cut c;
-  c.tiles_m = (M + kTile - 1) / kTile;
-  c.tiles_n = (cols + cols_per_tile - 1) / cols_per_tile;
-  const int64_t tiles = c.tiles_m * c.tiles_n, steps = (K + kBK - 1) / kBK;
+  c.direct = direct;
+  auto tiles = [&](int edge) {
+    const int64_t per = gated ? edge / 2 : edge;
+    c.tiles_m = (M + edge - 1) / edge;
+    c.tiles_n = (cols + per - 1) / per;
+    return c.tiles_m * c.tiles_n;
+  };
+  c.big = direct && tiles(256) >= cus;
+  const int64_t n = c.big ? c.tiles_m * c.tiles_n : tiles(128), steps = (K + kBK - 1) / kBK;
   int64_t s = 1;
-  if (tiles < 2 * cus) s = std::min<int64_t>(2 * cus / tiles, steps / 8);
+  if (n < 2 * cus && !c.big) s = std::min<int64_t>(2 * cus / n, steps / 8);
   s = std::max<int64_t>(1, s);
   const int64_t per = std::max<int64_t>(1, (steps + s - 1) / s);
   c.kslice = per * kBK;
   c.splits = static_cast<int>(std::max<int64_t>(1, (steps + per - 1) / per));
   return c;
+}
+
+// Operands that the loads to LDS fit: rows of whole 16-byte groups on 16-byte boundaries.
+bool direct_ok(const void* a, int64_t lda, const void* b, int64_t ldb) {
+  return lda % 8 == 0 && ldb % 8 == 0 && lda <= kMaxLd && ldb <= kMaxLd && aligned(a, 16) && aligned(b, 16);
 }
 
 template <int DT, bool AKM, bool BKM, bool GATED>
@@ -412,9 +570,14 @@ hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
   a.tiles_n = c.tiles_n;
   a.splits = c.splits;
   a.kslice = c.kslice;
-  const auto grid = static_cast<unsigned>(c.tiles_m * c.tiles_n * c.splits);
-  FPSK_LAUNCH((mm_kernel<DT, kTile, kTile, 2, 2, AKM, BKM, GATED>), dim3(grid), dim3(256), 0, st, a,
-              act);
+  const dim3 grid(static_cast<unsigned>(c.tiles_m * c.tiles_n * c.splits));
+  if (c.big) {
+    FPSK_LAUNCH((mm_kernel<DT, 256, 256, 2, 4, AKM, BKM, GATED>), grid, dim3(512), 0, st, a, act);
+  } else if (c.direct) {
+    FPSK_LAUNCH((mm_kernel<DT, 128, 128, 2, 2, AKM, BKM, GATED>), grid, dim3(256), 0, st, a, act);
+  } else {
+    FPSK_LAUNCH((mm_ragged_kernel<DT, 128, 128, 2, 2, AKM, BKM, GATED>), grid, dim3(256), 0, st, a, act);
+  }
   if (c.splits > 1) {
     const int64_t count = a.M * (GATED ? a.f : a.N);
     const auto g = static_cast<unsigned>(std::min<int64_t>((count + kThreads - 1) / kThreads, 8192));
@@ -452,7 +615,8 @@ extern "C" {
 int64_t fpsketch_gated_workspace(int64_t t, int64_t d, int64_t f) {
   int cus = 0;
   if (!dims_ok(t, d, f) || t == 0 || layer_device(&cus) != FPSK_OK) return 0;
-  return part_bytes(cut_of(t, f, kTile / 2, d, cus), t, 2 * f);
+  return std::max(part_bytes(cut_of(t, f, true, d, true, cus), t, 2 * f),
+                  part_bytes(cut_of(t, f, true, d, false, cus), t, 2 * f));
 }
 
 fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f,
@@ -469,7 +633,7 @@ fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t 
   int cus = 0;
   const fpsketch_status s = layer_device(&cus);
   if (s != FPSK_OK) return s;
-  const Cut c = cut_of(t, f, kTile / 2, d, cus);
+  const Cut c = cut_of(t, f, true, d, direct_ok(X, d, W, d), cus);
   const int64_t need = part_bytes(c, t, 2 * f);
   if (!launch_fits(c)) return layer_error(FPSK_ESHAPE, "fpsketch_gated: too many tiles");
   if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16))) {
@@ -556,8 +720,12 @@ int64_t fpsketch_gated_products_workspace(int64_t t, int64_t d, int64_t f) {
   int cus = 0;
   if (!dims_ok(t, d, f) || layer_device(&cus) != FPSK_OK) return 0;
   // the two products run one after the other and share it
-  const int64_t x = t > 0 ? part_bytes(cut_of(t, d, kTile, 2 * f, cus), t, d) : 0;
-  return std::max(x, part_bytes(cut_of(2 * f, d, kTile, t, cus), 2 * f, d));
+  int64_t n = 0;
+  for (const bool direct : {false, true}) {
+    if (t > 0) n = std::max(n, part_bytes(cut_of(t, d, false, 2 * f, direct, cus), t, d));
+    n = std::max(n, part_bytes(cut_of(2 * f, d, false, t, direct, cus), 2 * f, d));
+  }
+  return n;
 }
 
 fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const void* W, int64_t t,
@@ -577,8 +745,8 @@ fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const voi
   int cus = 0;
   const fpsketch_status s = layer_device(&cus);
   if (s != FPSK_OK) return s;
-  const Cut cx = cut_of(std::max<int64_t>(t, 1), d, kTile, 2 * f, cus);
-  const Cut cw = cut_of(2 * f, d, kTile, t, cus);
+  const Cut cx = cut_of(std::max<int64_t>(t, 1), d, false, 2 * f, direct_ok(dP, 2 * f, W, d), cus);
+  const Cut cw = cut_of(2 * f, d, false, t, direct_ok(dP, 2 * f, X, d), cus);
   int64_t need = 0;
   if (dX != nullptr && t > 0) need = part_bytes(cx, t, d);
   if (dW != nullptr) need = std::max(need, part_bytes(cw, 2 * f, d));
