@@ -245,18 +245,24 @@ struct Wave {
     }
   }
 
+  // One step.  A row block's fragment is read two blocks ahead of its products, the second half's
+  // fragments of B during the last blocks of the first; the barriers keep the scheduler from moving
+  // the reads down to their use, where the matrix cores would wait for LDS.
   __device__ __forceinline__ void multiply(const char* la, const char* lb) {
+    static_assert(MT >= NTL && MT > 2, "");
+    u32x4 fa[3], fb[2][NTL];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      u32x4 fb[NTL];
+    for (int j = 0; j < NTL; ++j) fb[0][j] = TB::frag(lb, wn + 16 * j, 0);
+    fa[0] = TA::frag(la, wm, 0);
+    fa[1] = TA::frag(la, wm + 16, 0);
 #pragma unroll
-      for (int j = 0; j < NTL; ++j) fb[j] = TB::frag(lb, wn + 16 * j, ks);
+    for (int g = 0; g < 2 * MT; ++g) {
+      const int ks = g / MT, i = g % MT, next = g + 2;
+      if (next < 2 * MT) fa[next % 3] = TA::frag(la, wm + 16 * (next % MT), next / MT);
+      if (ks == 0 && i >= MT - NTL) fb[1][i - (MT - NTL)] = TB::frag(lb, wn + 16 * (i - (MT - NTL)), 1);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const u32x4 fa = TA::frag(la, wm + 16 * i, ks);
-#pragma unroll
-        for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[j], fa, acc[i][j]);
-      }
+      for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[ks][j], fa[g % 3], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
