@@ -15,6 +15,7 @@
 #include "fpsk_layers.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fpsk {
 
@@ -120,19 +121,22 @@ struct Tile {
   }
 };
 
-// The same tile filled by loads that go straight to LDS: 16-byte groups on 16-byte boundaries (rows a
-// multiple of 8 long), 32-bit offsets within the tile (ld at most kMaxLd).  A wave's 64 groups land in
-// order, so the permutation is in the addresses.  Rows past the end repeat the last one, whose
-// products are not stored; k past K reads zeros.
+// A stage: the same tile KD deep, filled by loads that go straight to LDS: 16-byte groups on 16-byte
+// boundaries (rows a multiple of 8 long), 32-bit offsets within the tile (ld at most kMaxLd).  A
+// wave's 64 groups land in order, so the permutation is in the addresses.  Rows past the end repeat the last one, whose products
+// are not stored; for k past K the offset is one that the buffer's bounds turn into zeros.
 constexpr int64_t kMaxLd = int64_t{1} << 22;
+constexpr uint32_t kBound = 1u << 31, kOutside = ~15u;   // bytes of a buffer; an offset past them
 
-__device__ const u32x4 kZeros[4] = {};
-
-template <int R, int NT, bool KM, bool GATE>
-struct Direct {
-  static constexpr int kLoads = R * 8 / NT;
+template <int R, int NT, int KD, bool KM, bool GATE>
+struct Stage {
+  static_assert(KM || KD == kBK, "half a line of a row would come from L2 twice");
+  typedef Tile<R, NT, KM, GATE> T;
+  static constexpr int kBytes = R * KD * 2;
+  static constexpr int kLoads = R * KD / 8 / NT;
   static constexpr int kRows = 8 * NT / R;   // K-major: k rows per load
-  static_assert(NT % 128 == 0 && (KM ? kRows : NT / 8) % 16 == 0, "the permutation is the same for every load");
+  static_assert(kLoads >= 1 && NT % 128 == 0 && (KM ? kRows : NT / 8) % 16 == 0,
+                "the permutation is the same for every load");
   const char* base;        // the wave's tile at k = 0
   int64_t step;            // bytes from one k to the next
   uint32_t at[KM ? 1 : kLoads];
@@ -149,7 +153,7 @@ struct Direct {
     if constexpr (KM) {
       kk = L / (R / 8);
       const int slot = L % (R / 8);
-      const int c = (((slot >> 1) ^ Tile<R, NT, KM, GATE>::hash(kk)) << 1) | (slot & 1);
+      const int c = (((slot >> 1) ^ T::hash(kk)) << 1) | (slot & 1);
       at[0] = static_cast<uint32_t>(2 * (kk * ld + (r0 + 8 * c < rows ? 8 * c : rows - 8 - r0)));
     } else {
       const int c = (L & 7) ^ ((L >> 4) & 7);
@@ -163,18 +167,21 @@ struct Direct {
     }
   }
 
-  // The tile at k0; TAIL: zeros from K on.
-  template <bool TAIL>
+  // The stage at k0, zeros from K on (all of it where k0 >= K).
   __device__ __forceinline__ void load(char* lds, int64_t k0, int64_t K) const {
-    const char* from = base + k0 * step;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int left = static_cast<int>(K - k0 < KD ? K - k0 : KD);
+    // (past K the base itself must not run on: nothing is read there, but it stays an address)
+    const char* from = base + (left > 0 ? k0 : 0) * step;
+    const __amdgpu_buffer_rsrc_t buffer =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, kBound, 0x00027000);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const char* p = from + (KM ? i * static_cast<int64_t>(rows_on) : 0) + at[KM ? 0 : i];
-      if (TAIL && k0 + kk + (KM ? i * kRows : 0) >= K) p = reinterpret_cast<const char*>(kZeros);
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p),
-                                       (__attribute__((address_space(3))) void*)(lds + (i * NT + 64 * wave) * 16),
-                                       16, 0, 0);
+      const int k = kk + (KM ? i * kRows : 0);
+      const uint32_t o = at[KM ? 0 : i] + (KM ? i * rows_on : 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          buffer, (__attribute__((address_space(3))) void*)(lds + (i * NT + 64 * wave) * 16), 16,
+          k < left ? o : kOutside, 0, 0, 0);
     }
   }
 };
@@ -245,24 +252,18 @@ struct Wave {
     }
   }
 
-  // One step.  A row block's fragment is read two blocks ahead of its products, the second half's
-  // fragments of B during the last blocks of the first; the barriers keep the scheduler from moving
-  // the reads down to their use, where the matrix cores would wait for LDS.
   __device__ __forceinline__ void multiply(const char* la, const char* lb) {
-    static_assert(MT >= NTL && MT > 2, "");
-    u32x4 fa[3], fb[2][NTL];
 #pragma unroll
-    for (int j = 0; j < NTL; ++j) fb[0][j] = TB::frag(lb, wn + 16 * j, 0);
-    fa[0] = TA::frag(la, wm, 0);
-    fa[1] = TA::frag(la, wm + 16, 0);
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 fb[NTL];
 #pragma unroll
-    for (int g = 0; g < 2 * MT; ++g) {
-      const int ks = g / MT, i = g % MT, next = g + 2;
-      if (next < 2 * MT) fa[next % 3] = TA::frag(la, wm + 16 * (next % MT), next / MT);
-      if (ks == 0 && i >= MT - NTL) fb[1][i - (MT - NTL)] = TB::frag(lb, wn + 16 * (i - (MT - NTL)), 1);
+      for (int j = 0; j < NTL; ++j) fb[j] = TB::frag(lb, wn + 16 * j, ks);
 #pragma unroll
-      for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[ks][j], fa[g % 3], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < MT; ++i) {
+        const u32x4 fa = TA::frag(la, wm + 16 * i, ks);
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[j], fa, acc[i][j]);
+      }
     }
   }
 
@@ -366,60 +367,153 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_ragged_kernel(MmArgs a, in
   w.store(a, p.m0, p.n0, p.split, act);
 }
 
-// Waits for this wave's loads to LDS, then for the work-group: afterwards every wave's are there, and
-// every wave has done with the buffer that the next loads go to.
-__device__ __forceinline__ void loads_done() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
+// Waits until at most `left` of this wave's loads to LDS are under way, then for the work-group.
+template <int left>
+__device__ __forceinline__ void stages_ready() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(left) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
-// Whole 16-byte groups: the next step's tiles go straight to LDS during the products of this one.
+// Whole 16-byte groups, two buffers of 64 k: the next step's loads are under way during this one's
+// products.  A row block's fragment is read two blocks ahead of its products, the second half's
+// fragments of B during the last blocks of the first; the barriers keep the scheduler from moving
+// the reads down to their use, where the matrix cores would wait for LDS (796 -> 747 us at 4096 x
+// 4096 x 22016).  A buffer is an array of its own, so that the compiler knows loads into one apart
+// from reads of the other.
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) {
   typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
-  // one array a buffer, so that the compiler knows loads into one apart from reads of the other
-  __shared__ __attribute__((aligned(16))) char a0[W::TA::kBytes];
-  __shared__ __attribute__((aligned(16))) char b0[W::TB::kBytes];
-  __shared__ __attribute__((aligned(16))) char a1[W::TA::kBytes];
-  __shared__ __attribute__((aligned(16))) char b1[W::TB::kBytes];
+  typedef Stage<BM, W::NT, kBK, AKM, false> SA;
+  typedef Stage<BN, W::NT, kBK, BKM, GATED> SB;
+  constexpr int MT = W::MT, NTL = W::NTL;
+  static_assert(MT >= NTL && MT > 2, "");
+  __shared__ __attribute__((aligned(16))) char a0[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char b0[SB::kBytes];
+  __shared__ __attribute__((aligned(16))) char a1[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char b1[SB::kBytes];
   const Part p = part_of<BM, BN, GATED>(a);
-  Direct<BM, W::NT, AKM, false> da;
-  Direct<BN, W::NT, BKM, GATED> db;
-  da.init(a.A, p.m0, a.M, AKM ? a.M : a.K, 0);
-  db.init(a.B, p.n0, a.N, BKM ? a.N : a.K, a.f);
+  SA sa;
+  SB sb;
+  sa.init(a.A, p.m0, a.M, AKM ? a.M : a.K, 0);
+  sb.init(a.B, p.n0, a.N, BKM ? a.N : a.K, a.f);
   W w;
   w.init();
   auto load = [&](char* la, char* lb, int64_t k) {
-    da.template load<false>(la, k, p.k1);
-    db.template load<false>(lb, k, p.k1);
+    sa.load(la, k, p.k1);
+    sb.load(lb, k, p.k1);
     __builtin_amdgcn_sched_barrier(0);     // (else the loads sink to the end of the products)
   };
-  // Whole steps; the last one is loaded again where no other follows.
-  int64_t n = (p.k1 - p.k0) / kBK, k = p.k0;
-  const int64_t last = p.k0 + (n - 1) * kBK;
-  if (n > 0) {
-    load(a0, b0, k);
-    for (; n > 1; n -= 2, k += 2 * kBK) {
-      loads_done();
-      load(a1, b1, k + kBK);
-      w.multiply(a0, b0);
-      loads_done();
-      load(a0, b0, k + 2 * kBK < last ? k + 2 * kBK : last);
-      w.multiply(a1, b1);
+  auto multiply = [&](const char* la, const char* lb) {
+    u32x4 fa[3], fb[2][NTL];
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) fb[0][j] = W::TB::frag(lb, w.wn + 16 * j, 0);
+    fa[0] = W::TA::frag(la, w.wm, 0);
+    fa[1] = W::TA::frag(la, w.wm + 16, 0);
+#pragma unroll
+    for (int g = 0; g < 2 * MT; ++g) {
+      const int ks = g / MT, i = g % MT, next = g + 2;
+      if (next < 2 * MT) fa[next % 3] = W::TA::frag(la, w.wm + 16 * (next % MT), next / MT);
+      if (ks == 0 && i >= MT - NTL) fb[1][i - (MT - NTL)] = W::TB::frag(lb, w.wn + 16 * (i - (MT - NTL)), 1);
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) w.acc[i][j] = mfma32<DT>(fb[ks][j], fa[g % 3], w.acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    loads_done();                          // also where nothing is left: no load outlives the kernel
-    if (n == 1) {
-      w.multiply(a0, b0);
-      k += kBK;
-    }
+  };
+  load(a0, b0, p.k0);
+  int64_t k = p.k0;
+  for (; k + kBK < p.k1; k += 2 * kBK) {   // (loads past K fill a buffer with zeros)
+    stages_ready<0>();
+    load(a1, b1, k + kBK);
+    multiply(a0, b0);
+    stages_ready<0>();
+    load(a0, b0, k + 2 * kBK);
+    multiply(a1, b1);
   }
-  if (k < p.k1) {                          // the broken step (every wave has left a1 and b1)
-    da.template load<true>(a1, k, p.k1);
-    db.template load<true>(b1, k, p.k1);
-    loads_done();
-    w.multiply(a1, b1);
-  }
+  stages_ready<0>();                       // no load outlives the kernel
+  if (k < p.k1) multiply(a0, b0);
   w.store(a, p.m0, p.n0, p.split, act);
+}
+
+// Both operands K-major (dW): five stages of 32 k, stage s in buffer s % 5.  While one is multiplied
+// the next is there already, so that its first fragments are read before the barrier, and three are
+// under way; the stages past K that fill the last turn hold zeros.  22016 x 4096 x 2048: 383 us with
+// two buffers of 64 k, 364 us.  (A row-major operand would read half a line per stage: 747 -> 781 us
+// at 4096 x 4096 x 22016, and 912 us with the halves of a line loaded together.)
+template <int DT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mm_deep_kernel(MmArgs a) {
+  typedef Wave<DT, BM, BN, WM, WN, true, true, false> W;
+  constexpr int KD = 32;
+  typedef Stage<BM, W::NT, KD, true, false> SA;
+  typedef Stage<BN, W::NT, KD, true, false> SB;
+  constexpr int MT = W::MT, NTL = W::NTL, kStageLoads = SA::kLoads + SB::kLoads;
+  static_assert(MT >= NTL, "");
+  __shared__ __attribute__((aligned(16))) char a0[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char a1[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char a2[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char a3[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char a4[SA::kBytes];
+  __shared__ __attribute__((aligned(16))) char b0[SB::kBytes];
+  __shared__ __attribute__((aligned(16))) char b1[SB::kBytes];
+  __shared__ __attribute__((aligned(16))) char b2[SB::kBytes];
+  __shared__ __attribute__((aligned(16))) char b3[SB::kBytes];
+  __shared__ __attribute__((aligned(16))) char b4[SB::kBytes];
+  const Part p = part_of<BM, BN, false>(a);
+  SA sa;
+  SB sb;
+  sa.init(a.A, p.m0, a.M, a.M, 0);
+  sb.init(a.B, p.n0, a.N, a.N, 0);
+  W w;
+  w.init();
+  auto load = [&](char* la, char* lb, int64_t k) {
+    sa.load(la, k, p.k1);
+    sb.load(lb, k, p.k1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  u32x4 fa[2], fb[NTL];                    // the first two row blocks and all of B
+  // Multiplies the stage at la, lb and reads the first fragments of the next from na, nb; the loads
+  // at k go to where the stage before was, oa, ob.
+  auto step = [&](const char* la, const char* na, const char* nb, char* oa, char* ob, int64_t k) {
+    stages_ready<2 * kStageLoads>();
+    load(oa, ob, k);
+    u32x4 f[3], ga[2], gb[NTL];
+    f[0] = fa[0];
+    f[1] = fa[1];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      if (i + 2 < MT) {
+        f[(i + 2) % 3] = W::TA::frag(la, w.wm + 16 * (i + 2), 0);
+      } else {
+        ga[i + 2 - MT] = W::TA::frag(na, w.wm + 16 * (i + 2 - MT), 0);
+      }
+      if (i >= MT - NTL) gb[i - (MT - NTL)] = W::TB::frag(nb, w.wn + 16 * (i - (MT - NTL)), 0);
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) w.acc[i][j] = mfma32<DT>(fb[j], f[i % 3], w.acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    fa[0] = ga[0];
+    fa[1] = ga[1];
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) fb[j] = gb[j];
+  };
+  load(a0, b0, p.k0);
+  load(a1, b1, p.k0 + KD);
+  load(a2, b2, p.k0 + 2 * KD);
+  load(a3, b3, p.k0 + 3 * KD);
+  stages_ready<3 * kStageLoads>();
+  fa[0] = W::TA::frag(a0, w.wm, 0);
+  fa[1] = W::TA::frag(a0, w.wm + 16, 0);
+#pragma unroll
+  for (int j = 0; j < NTL; ++j) fb[j] = W::TB::frag(b0, w.wn + 16 * j, 0);
+  for (int64_t k = p.k0; k < p.k1; k += 5 * KD) {
+    step(a0, a1, b1, a4, b4, k + 4 * KD);
+    step(a1, a2, b2, a0, b0, k + 5 * KD);
+    step(a2, a3, b3, a1, b1, k + 6 * KD);
+    step(a3, a4, b4, a2, b2, k + 7 * KD);
+    step(a4, a0, b0, a3, b3, k + 8 * KD);
+  }
+  stages_ready<0>();                       // no load outlives the kernel
+  w.store(a, p.m0, p.n0, p.split, 0);
 }
 
 // A product with an operand of fewer than 8 elements, which 16-byte loads do not fit: one output
@@ -529,8 +623,9 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, cons
 
 // ---- host ------------------------------------------------------------------------------------
 
-// How a product is cut: tiles of 256 x 256 where they fill the chip, else of 128 x 128, with K in
-// parts while those would not fill it twice over and every part keeps at least 8 steps.
+// How a product is cut: tiles of 256 x 256 where they fill the chip, if need be with K in up to 4
+// parts of at least 32 steps; else of 128 x 128, with K in parts while those would not fill it twice
+// over and every part keeps at least 8 steps.
 struct Cut {
   bool big, direct;
   int64_t tiles_m, tiles_n, kslice;
@@ -547,10 +642,13 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, int64_t K, bool direct, int cus)
     c.tiles_n = (cols + per - 1) / per;
     return c.tiles_m * c.tiles_n;
   };
-  c.big = direct && tiles(256) >= cus;
-  const int64_t n = c.big ? c.tiles_m * c.tiles_n : tiles(128), steps = (K + kBK - 1) / kBK;
-  int64_t s = 1;
-  if (n < 2 * cus && !c.big) s = std::min<int64_t>(2 * cus / n, steps / 8);
+  const int64_t steps = (K + kBK - 1) / kBK, large = tiles(256);
+  int64_t s = large >= cus ? 1 : (cus + large - 1) / large;
+  c.big = direct && (large >= cus || (s <= 4 && steps >= 32 * s));
+  if (!c.big) {
+    const int64_t n = tiles(128);
+    s = n < 2 * cus ? std::min<int64_t>(2 * cus / n, steps / 8) : 1;
+  }
   s = std::max<int64_t>(1, s);
   const int64_t per = std::max<int64_t>(1, (steps + s - 1) / s);
   c.kslice = per * kBK;
@@ -578,7 +676,11 @@ hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
   a.kslice = c.kslice;
   const dim3 grid(static_cast<unsigned>(c.tiles_m * c.tiles_n * c.splits));
   if (c.big) {
-    FPSK_LAUNCH((mm_kernel<DT, 256, 256, 2, 4, AKM, BKM, GATED>), grid, dim3(512), 0, st, a, act);
+    if constexpr (AKM && BKM) {
+      FPSK_LAUNCH((mm_deep_kernel<DT, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
+    } else {
+      FPSK_LAUNCH((mm_kernel<DT, 256, 256, 2, 4, AKM, BKM, GATED>), grid, dim3(512), 0, st, a, act);
+    }
   } else if (c.direct) {
     FPSK_LAUNCH((mm_kernel<DT, 128, 128, 2, 2, AKM, BKM, GATED>), grid, dim3(256), 0, st, a, act);
   } else {
