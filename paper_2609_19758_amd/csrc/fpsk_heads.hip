@@ -36,7 +36,7 @@ struct HeadArgs {
   const uint16_t* dk;
   const uint16_t* dv;
   uint16_t* dC;
-  float* part;             // work-groups x 2 x hd partial gain gradients (q, k)
+  float* part;             // 2 x hd x work-groups: partial gain gradients (q, k)
   float* dgq;
   float* dgk;
   int groups;
@@ -58,7 +58,222 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// One token per work-group, one head per wave at a time.
+// Heads whose entries come in whole groups: hd and rd multiples of 8 (loads and stores of 8 and 16
+// bytes at element alignment, which gfx950 takes).  LPH lanes take a head, 8 entries each: the groups of 4 that rotate with each other (4u and rd / 2 + 4u, or
+// 8u and 8u + 4 with interleaved pairs), or 8 neighbours past rd.  A lane meets the same entries in
+// every head, so gains and angles stay in its registers, and nothing passes through LDS.
+struct Unit {
+  int e0, e1;              // its groups of 4
+  bool turns;
+};
+
+__device__ __forceinline__ Unit unit_of(const HeadArgs& a, int u) {
+  if (!a.inter && 8 * u < a.rd) return {4 * u, a.rd / 2 + 4 * u, true};
+  return {8 * u, 8 * u + 4, 8 * u < a.rd};
+}
+
+template <int LPH>
+__device__ __forceinline__ float head_sum(float v) {
+#pragma unroll
+  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// (x0, x1) turned by the angles of (c, s): pairs (x0[e], x1[e]), or neighbours.
+__device__ __forceinline__ void turn(bool inter, f32x4 c, f32x4 s, f32x4& x0, f32x4& x1) {
+  if (inter) {
+    const f32x4 a = x0, b = x1;
+    x0 = f32x4{a[0] * c[0] - a[1] * s[0], a[1] * c[0] + a[0] * s[0], a[2] * c[1] - a[3] * s[1], a[3] * c[1] + a[2] * s[1]};
+    x1 = f32x4{b[0] * c[2] - b[1] * s[2], b[1] * c[2] + b[0] * s[2], b[2] * c[3] - b[3] * s[3], b[3] * c[3] + b[2] * s[3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float p = x0[e], q = x1[e];
+      x0[e] = p * c[e] - q * s[e];
+      x1[e] = q * c[e] + p * s[e];
+    }
+  }
+}
+
+__device__ __forceinline__ void unit_angles(const HeadArgs& a, int64_t i, int u, f32x4& c, f32x4& s) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x, y;
+    angle(a.pos[i], a.freq[4 * u + e], &x, &y);
+    c[e] = x;
+    s[e] = y;
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void put4(uint16_t* y, f32x4 x) {
+  *reinterpret_cast<u16x4_a2*>(y) = to_half4<DT>(x[0], x[1], x[2], x[3]);
+}
+
+// One token per work-group, or part of its heads (gridDim.y parts): bound by reading C and writing
+// the heads.  A wave takes 64 / LPH heads at a time, the next ones under way.
+template <int DT, int LPH, bool NORM>
+__global__ __launch_bounds__(kThreads) void heads_vec_kernel(HeadArgs a) {
+  constexpr int HPW = 64 / LPH;
+  const int lane = threadIdx.x & 63, u = lane % LPH, units = a.hd / 8;
+  const int nq = a.hq, nk = a.hq + a.hkv, width = a.hq + 2 * a.hkv;
+  const int step = 4 * gridDim.y * HPW;
+  const int h0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * HPW + lane / LPH;
+  const bool live = u < units;
+  const Unit t = unit_of(a, live ? u : 0);
+  f32x4 gq[2], gk[2];
+  if constexpr (NORM) {
+    gq[0] = *reinterpret_cast<const f32x4_a4*>(a.gq + t.e0);
+    gq[1] = *reinterpret_cast<const f32x4_a4*>(a.gq + t.e1);
+    gk[0] = *reinterpret_cast<const f32x4_a4*>(a.gk + t.e0);
+    gk[1] = *reinterpret_cast<const f32x4_a4*>(a.gk + t.e1);
+  }
+  for (int64_t i = blockIdx.x; i < a.t; i += gridDim.x) {
+    const float* row = a.C + i * width * a.hd;
+    f32x4 n0, n1;
+    auto fetch = [&](int h) {                // (past the last head: that one again)
+      const float* x = row + static_cast<int64_t>(h < width ? h : width - 1) * a.hd;
+      n0 = *reinterpret_cast<const f32x4_a4*>(x + t.e0);
+      n1 = *reinterpret_cast<const f32x4_a4*>(x + t.e1);
+    };
+    fetch(h0);
+    f32x4 c = {1.0f, 1.0f, 1.0f, 1.0f}, s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (t.turns) unit_angles(a, i, u, c, s);
+    for (int h = h0; h - lane / LPH < width; h += step) {
+      f32x4 x0 = n0, x1 = n1;
+      fetch(h + step);
+      if constexpr (NORM) {
+        float ss = 0.0f;
+        if (live) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
+        }
+        const float r = 1.0f / sqrtf(head_sum<LPH>(ss) / static_cast<float>(a.hd) + a.eps);
+        if (h < nk) {
+          x0 *= r * (h < nq ? gq[0] : gk[0]);
+          x1 *= r * (h < nq ? gq[1] : gk[1]);
+        }
+      }
+      if (h < nk && t.turns) turn(a.inter, c, s, x0, x1);
+      if (!live || h >= width) continue;
+      uint16_t* y = h < nq   ? a.q + (i * a.hq + h) * a.hd
+                    : h < nk ? a.k + (i * a.hkv + h - nq) * a.hd
+                             : a.v + (i * a.hkv + h - nk) * a.hd;
+      put4<DT>(y + t.e0, x0);
+      put4<DT>(y + t.e1, x1);
+    }
+  }
+}
+
+// The backward pass likewise; a lane sums its entries of the gains' gradients over all its heads, the
+// work-group's lanes meet in LDS at the end.
+template <int DT, int LPH, bool NORM>
+__global__ __launch_bounds__(kThreads) void heads_grad_vec_kernel(HeadArgs a) {
+  constexpr int HPW = 64 / LPH;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, u = lane % LPH, units = a.hd / 8;
+  const int nq = a.hq, nk = a.hq + a.hkv, width = a.hq + 2 * a.hkv;
+  const int h0 = wave * HPW + lane / LPH;
+  const bool live = u < units;
+  const Unit t = unit_of(a, live ? u : 0);
+  f32x4 gq[2], gk[2], dq[2] = {}, dk[2] = {};
+  if constexpr (NORM) {
+    gq[0] = *reinterpret_cast<const f32x4_a4*>(a.gq + t.e0);
+    gq[1] = *reinterpret_cast<const f32x4_a4*>(a.gq + t.e1);
+    gk[0] = *reinterpret_cast<const f32x4_a4*>(a.gk + t.e0);
+    gk[1] = *reinterpret_cast<const f32x4_a4*>(a.gk + t.e1);
+  }
+  for (int64_t i = blockIdx.x; i < a.t; i += gridDim.x) {
+    f32x4 n0 = {}, n1 = {};
+    u16x4 m0, m1;
+    auto fetch = [&](int h_) {               // (past the last head: that one again; C has no use in v)
+      const int h = h_ < width ? h_ : width - 1;
+      const uint16_t* dy = h < nq   ? a.dq + (i * a.hq + h) * a.hd
+                           : h < nk ? a.dk + (i * a.hkv + h - nq) * a.hd
+                                    : a.dv + (i * a.hkv + h - nk) * a.hd;
+      m0 = *reinterpret_cast<const u16x4_a2*>(dy + t.e0);
+      m1 = *reinterpret_cast<const u16x4_a2*>(dy + t.e1);
+      if constexpr (NORM) {
+        const float* x = a.C + (i * width + (h < nk ? h : nk - 1)) * a.hd;
+        n0 = *reinterpret_cast<const f32x4_a4*>(x + t.e0);
+        n1 = *reinterpret_cast<const f32x4_a4*>(x + t.e1);
+      }
+    };
+    fetch(h0);
+    f32x4 c = {1.0f, 1.0f, 1.0f, 1.0f}, s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (t.turns) unit_angles(a, i, u, c, s);
+    for (int h = h0; h - lane / LPH < width; h += 4 * HPW) {
+      const f32x4 x0 = n0, x1 = n1;
+      const u16x4 y0 = m0, y1 = m1;
+      fetch(h + 4 * HPW);
+      f32x4 u0, u1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        u0[e] = from_half<DT>(y0[e]);
+        u1[e] = from_half<DT>(y1[e]);
+      }
+      if (h < nk && t.turns) turn(a.inter, c, -s, u0, u1);
+      if constexpr (NORM) {
+        const f32x4 g0 = h < nq ? gq[0] : gk[0], g1 = h < nq ? gq[1] : gk[1];
+        float ss = 0.0f, xu = 0.0f;
+        if (live) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            ss += x0[e] * x0[e] + x1[e] * x1[e];
+            xu += x0[e] * g0[e] * u0[e] + x1[e] * g1[e] * u1[e];
+          }
+        }
+        const float n = static_cast<float>(a.hd);
+        const float r = 1.0f / sqrtf(head_sum<LPH>(ss) / n + a.eps);
+        const float f = r * r * head_sum<LPH>(xu) / n;
+        if (h < nk) {
+          const f32x4 d0 = u0 * x0 * r, d1 = u1 * x1 * r;
+          if (h < nq) {
+            dq[0] += d0;
+            dq[1] += d1;
+          } else {
+            dk[0] += d0;
+            dk[1] += d1;
+          }
+          u0 = r * (g0 * u0 - x0 * f);
+          u1 = r * (g1 * u1 - x1 * f);
+        }
+      }
+      if (!live || h >= width) continue;
+      uint16_t* dx = a.dC + (i * width + h) * a.hd;
+      if (h < nk) {
+        put4<DT>(dx + t.e0, u0);
+        put4<DT>(dx + t.e1, u1);
+      } else {
+        *reinterpret_cast<u16x4_a2*>(dx + t.e0) = y0;
+        *reinterpret_cast<u16x4_a2*>(dx + t.e1) = y1;
+      }
+    }
+  }
+  if constexpr (NORM) {
+    __shared__ float sums[4][2][kMaxHead];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        f32x4 d = w == 0 ? dq[b] : dk[b];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int o = LPH; o < 64; o <<= 1) d[e] += __shfl_xor(d[e], o, 64);
+          if (live && lane < LPH) sums[wave][w][(b == 0 ? t.e0 : t.e1) + e] = d[e];
+        }
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 2 * a.hd; e += kThreads) {
+      const int w = e / a.hd, j = e % a.hd;
+      a.part[static_cast<int64_t>(e) * a.groups + blockIdx.x] =
+          (sums[0][w][j] + sums[1][w][j]) + (sums[2][w][j] + sums[3][w][j]);
+    }
+  }
+}
+
+// Any head size: one token per work-group, one head per wave at a time.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void heads_kernel(HeadArgs a) {
   __shared__ float cs[kMaxHead / 2], sn[kMaxHead / 2];
@@ -160,16 +375,16 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadArgs a) {
   __syncthreads();
   for (int e = threadIdx.x; e < 2 * a.hd; e += kThreads) {
     const int w = e / a.hd, j = e % a.hd;
-    a.part[static_cast<int64_t>(blockIdx.x) * 2 * a.hd + e] =
+    a.part[static_cast<int64_t>(e) * a.groups + blockIdx.x] =
         (sums[0][w][j] + sums[1][w][j]) + (sums[2][w][j] + sums[3][w][j]);
   }
 }
 
-// The gains' gradients: the work-groups' sums in order, one entry per wave.
+// The gains' gradients: the work-groups' sums, one entry per wave.
 __global__ __launch_bounds__(64) void gains_kernel(HeadArgs a) {
   const int e = blockIdx.x, lane = threadIdx.x;
   double s = 0.0;
-  for (int g = lane; g < a.groups; g += 64) s += a.part[static_cast<int64_t>(g) * 2 * a.hd + e];
+  for (int g = lane; g < a.groups; g += 64) s += a.part[static_cast<int64_t>(e) * a.groups + g];
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if (lane == 0) {
     if (e < a.hd) {
@@ -181,6 +396,35 @@ __global__ __launch_bounds__(64) void gains_kernel(HeadArgs a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------
+
+// Whole groups: what the vector kernels take.
+bool whole(int hd, int rd) { return hd % 8 == 0 && rd % 8 == 0; }
+
+template <int DT, int LPH>
+hipError_t launch_vec(const HeadArgs& a, bool backward, dim3 grid, hipStream_t st) {
+  if (backward) {
+    if (a.gq != nullptr) return launch_k(heads_grad_vec_kernel<DT, LPH, true>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+    return launch_k(heads_grad_vec_kernel<DT, LPH, false>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+  }
+  if (a.gq != nullptr) return launch_k(heads_vec_kernel<DT, LPH, true>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+  return launch_k(heads_vec_kernel<DT, LPH, false>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+}
+
+int lanes_of(int hd) { return hd <= 64 ? 8 : hd <= 128 ? 16 : hd <= 256 ? 32 : 64; }
+
+template <int DT>
+hipError_t launch_heads(const HeadArgs& a, bool backward, bool vec, dim3 grid, hipStream_t st) {
+  if (!vec) {
+    if (backward) return launch_k(heads_grad_kernel<DT>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+    return launch_k(heads_kernel<DT>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+  }
+  switch (lanes_of(a.hd)) {
+    case 8: return launch_vec<DT, 8>(a, backward, grid, st);
+    case 16: return launch_vec<DT, 16>(a, backward, grid, st);
+    case 32: return launch_vec<DT, 32>(a, backward, grid, st);
+    default: return launch_vec<DT, 64>(a, backward, grid, st);
+  }
+}
 
 bool heads_dims(int64_t t, int hq, int hkv, int hd) {
   return t >= 0 && t < kDimLimit && hq >= 1 && hkv >= 1 && hd >= 1 && hd <= kMaxHead &&
@@ -255,10 +499,16 @@ fpsketch_status fpsketch_heads(const float* C, int64_t t, int32_t hq, int32_t hk
   a.k = static_cast<uint16_t*>(k);
   a.v = static_cast<uint16_t*>(v);
   const auto st = static_cast<hipStream_t>(stream);
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(t, 1 << 20)));
-  return launched(dtype == FPSK_BF16
-                      ? launch_k(heads_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a)
-                      : launch_k(heads_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a),
+  const bool vec = whole(hd, rd);
+  dim3 grid(static_cast<unsigned>(std::min<int64_t>(t, 1 << 20)));
+  if (vec && t < 4 * cus) {
+    // few tokens: a work-group for every round of heads, as long as that leaves each 8 work-groups
+    // a compute unit at most
+    const int rounds = (hq + 2 * hkv + 4 * (64 / lanes_of(hd)) - 1) / (4 * (64 / lanes_of(hd)));
+    grid.y = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(rounds, 8 * cus / t)));
+  }
+  return launched(dtype == FPSK_BF16 ? launch_heads<1>(a, false, vec, grid, st)
+                                     : launch_heads<0>(a, false, vec, grid, st),
                   "fpsketch_heads");
 }
 
@@ -323,9 +573,8 @@ fpsketch_status fpsketch_heads_grad(const void* dq, const void* dk, const void* 
   hipError_t e = hipSuccess;
   if (t > 0) {
     const dim3 grid(static_cast<unsigned>(groups));
-    e = dtype == FPSK_BF16
-            ? launch_k(heads_grad_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a)
-            : launch_k(heads_grad_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a);
+    const bool vec = whole(hd, rd);
+    e = dtype == FPSK_BF16 ? launch_heads<1>(a, true, vec, grid, st) : launch_heads<0>(a, true, vec, grid, st);
   }
   if (e == hipSuccess && norm) {
     e = launch_k(gains_kernel, dim3(static_cast<unsigned>(2 * hd)), dim3(64), 0, st, nullptr, nullptr, a);

@@ -16,6 +16,7 @@ namespace fpsk {
 fpsketch_status layer_error(fpsketch_status s, const char* detail) noexcept;
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef u16x4 u16x4_a2 __attribute__((aligned(2)));
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
