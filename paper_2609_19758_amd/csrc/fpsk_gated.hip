@@ -668,44 +668,101 @@ __device__ __forceinline__ void grads(float g, float u, float dh, float* dg, flo
   *du = dh * g * s;
 }
 
-// dP of a 32 x 32 block of H; the transpose goes through LDS so that its rows are written whole.
-template <int DT>
-__global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, const float* P,
-                                                        int64_t t, int64_t f, int act,
-                                                        uint16_t* dP, uint16_t* dPt,
+// dP of a 64 x 64 block of H: bound by its loads and stores (14 bytes an entry of H, 18 with the
+// transpose).  A thread takes 4 x 4 entries, all loads at once, and turns them in registers for the
+// transpose, whose rows then leave LDS as whole lines.
+template <int DT, int ACT>
+__global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, const float* P, int64_t t,
+                                                        int64_t f, uint16_t* dP, uint16_t* dPt,
                                                         int64_t blocks_f) {
-  __shared__ uint16_t tile[2][32][33];
-  const int64_t m0 = (blockIdx.x / blocks_f) * 32, j0 = (blockIdx.x % blocks_f) * 32;
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  for (int r = y; r < 32; r += 8) {
-    const int64_t m = m0 + r, j = j0 + x;
-    if (m < t && j < f) {
-      const int64_t at = 2 * m * f + j;
-      const float g = P[at], u = P[at + f], dh = from_half<DT>(dH[m * f + j]);
-      float dg, du;
-      if (act == 0) {
-        grads<0>(g, u, dh, &dg, &du);
-      } else if (act == 1) {
-        grads<1>(g, u, dh, &dg, &du);
-      } else {
-        grads<2>(g, u, dh, &dg, &du);
+  constexpr int kEdge = 64;
+  __shared__ __attribute__((aligned(16))) uint16_t tile[2][kEdge][kEdge + 4];   // columns x tokens
+  const int64_t m0 = (blockIdx.x / blocks_f) * kEdge, j0 = (blockIdx.x % blocks_f) * kEdge;
+  const int x = 4 * (threadIdx.x & 15), y = 4 * (threadIdx.x >> 4);
+  const bool full = m0 + kEdge <= t && j0 + kEdge <= f;
+  f32x4 g[4], u[4];
+  u16x4 h[4];
+  if (full) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t m = m0 + y + r, at = 2 * m * f + j0 + x;
+      g[r] = *reinterpret_cast<const f32x4_a4*>(P + at);
+      u[r] = *reinterpret_cast<const f32x4_a4*>(P + at + f);
+      h[r] = *reinterpret_cast<const u16x4_a2*>(dH + m * f + j0 + x);
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t m = m0 + y + r, j = j0 + x + e;
+        const bool in = m < t && j < f;
+        g[r][e] = in ? P[2 * m * f + j] : 0.0f;
+        u[r][e] = in ? P[2 * m * f + f + j] : 0.0f;
+        h[r][e] = in ? dH[m * f + j] : uint16_t{0};
       }
-      const uint16_t hg = to_half<DT>(dg), hu = to_half<DT>(du);
-      dP[at] = hg;
-      dP[at + f] = hu;
-      tile[0][r][x] = hg;
-      tile[1][r][x] = hu;
+    }
+  }
+  u16x4 hg[4], hu[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float dg, du;
+      grads<ACT>(g[r][e], u[r][e], from_half<DT>(h[r][e]), &dg, &du);
+      hg[r][e] = to_half<DT>(dg);
+      hu[r][e] = to_half<DT>(du);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t m = m0 + y + r, at = 2 * m * f + j0 + x;
+    if (full) {
+      *reinterpret_cast<u16x4_a2*>(dP + at) = hg[r];
+      *reinterpret_cast<u16x4_a2*>(dP + at + f) = hu[r];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (m < t && j0 + x + e < f) {
+          dP[at + e] = hg[r][e];
+          dP[at + f + e] = hu[r][e];
+        }
+      }
     }
   }
   if (dPt == nullptr) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    *reinterpret_cast<u16x4*>(&tile[0][x + e][y]) = u16x4{hg[0][e], hg[1][e], hg[2][e], hg[3][e]};
+    *reinterpret_cast<u16x4*>(&tile[1][x + e][y]) = u16x4{hu[0][e], hu[1][e], hu[2][e], hu[3][e]};
+  }
   __syncthreads();
-  for (int r = y; r < 32; r += 8) {
-    const int64_t j = j0 + r, m = m0 + x;
-    if (m < t && j < f) {
-      dPt[j * t + m] = tile[0][x][r];
-      dPt[(j + f) * t + m] = tile[1][x][r];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int half = i & 1, c = (threadIdx.x >> 4) + 16 * (i >> 1);
+    const u16x4 v = *reinterpret_cast<const u16x4*>(&tile[half][c][x]);
+    const int64_t j = j0 + c, m = m0 + x;
+    uint16_t* to = dPt + (j + half * f) * t + m;
+    if (full) {
+      *reinterpret_cast<u16x4_a2*>(to) = v;
+    } else if (j < f) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (m + e < t) to[e] = v[e];
+      }
     }
   }
+}
+
+template <int DT>
+hipError_t launch_grad(const uint16_t* dH, const float* P, int64_t t, int64_t f, int act, uint16_t* dP,
+                       uint16_t* dPt, hipStream_t st) {
+  const int64_t bf = (f + 63) / 64;
+  const dim3 grid(static_cast<unsigned>(bf * ((t + 63) / 64)));
+  if (act == FPSK_SILU) FPSK_LAUNCH((grad_kernel<DT, 0>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bf);
+  if (act == FPSK_GELU) FPSK_LAUNCH((grad_kernel<DT, 1>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bf);
+  if (act == FPSK_GELU_TANH) FPSK_LAUNCH((grad_kernel<DT, 2>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bf);
+  return hipSuccess;
 }
 
 // ---- host ------------------------------------------------------------------------------------
@@ -911,17 +968,14 @@ fpsketch_status fpsketch_gated_grad(const void* dH, const float* P, int64_t t, i
   const Span in[] = {{dH, 2 * t * f}, {P, 8 * t * f}};
   const Span out[] = {{dP, 4 * t * f}, {dPt, 4 * t * f}};
   if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated_grad: an output overlaps another argument");
-  const int64_t bf = (f + 31) / 32, blocks = bf * ((t + 31) / 32);
-  if (blocks >= int64_t{1} << 24) return layer_error(FPSK_ESHAPE, "fpsketch_gated_grad: too many blocks");
+  if (static_cast<double>((f + 63) / 64) * ((t + 63) / 64) * kThreads >= 4294967296.0) {
+    return layer_error(FPSK_ESHAPE, "fpsketch_gated_grad: too many blocks");
+  }
   const auto st = static_cast<hipStream_t>(stream);
   const auto* dh = static_cast<const uint16_t*>(dH);
   auto *o = static_cast<uint16_t*>(dP), *ot = static_cast<uint16_t*>(dPt);
-  const dim3 grid(static_cast<unsigned>(blocks));
-  return launched(dtype == FPSK_BF16
-                      ? launch_k(grad_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, dh, P, t,
-                                 f, static_cast<int>(act), o, ot, bf)
-                      : launch_k(grad_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, dh, P, t,
-                                 f, static_cast<int>(act), o, ot, bf),
+  return launched(dtype == FPSK_BF16 ? launch_grad<1>(dh, P, t, f, act, o, ot, st)
+                                     : launch_grad<0>(dh, P, t, f, act, o, ot, st),
                   "fpsketch_gated_grad");
 }
 

@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kThreads) void heads_vec_kernel(HeadArgs a) {
 // The backward pass likewise; a lane sums its entries of the gains' gradients over all its heads, the
 // work-group's lanes meet in LDS at the end.
 template <int DT, int LPH, bool NORM>
-__global__ __launch_bounds__(kThreads) void heads_grad_vec_kernel(HeadArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void heads_grad_vec_kernel(HeadArgs a) {
   constexpr int HPW = 64 / LPH;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, u = lane % LPH, units = a.hd / 8;
   const int nq = a.hq, nk = a.hq + a.hkv, width = a.hq + 2 * a.hkv;
