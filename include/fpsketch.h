@@ -346,7 +346,7 @@ double fpsketch_rms_hat_samples(const float* samples, int64_t count);
 /* `stream` is done, so calls that may overlap in time (other streams, graphs replayed beside  */
 /* each other) each need their own.  Sums, products and statistics are held in FP32 or more,   */
 /* and each result is rounded once.  FPSK_ESHAPE: a dimension outside [1, 2^31) (t: [0, 2^31)) */
-/* or an array of more than 2^40 elements; FPSK_EINVAL: null or misaligned pointers and the    */
+/* (gated block: d and 2f at most 2^22) or an array of more than 2^40 elements; FPSK_EINVAL: null or misaligned pointers and the    */
 /* rest.                                                                                       */
 
 typedef enum { FPSK_SILU = 0, FPSK_GELU = 1, FPSK_GELU_TANH = 2 } fpsketch_act;
@@ -359,7 +359,7 @@ typedef enum { FPSK_PAIRS_HALF = 0, FPSK_PAIRS_INTERLEAVED = 1 } fpsketch_pairs;
 fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f,
                                fpsketch_dtype dtype, fpsketch_act act, void* H, float* P,
                                void* workspace, int64_t workspace_bytes, void* stream);
-int64_t fpsketch_gated_workspace(int64_t t, int64_t d, int64_t f);
+int64_t fpsketch_gated_workspace(const void* X, const void* W, int64_t t, int64_t d, int64_t f);
 
 /* H = act(G) U from a delivered product, for instance after fpsketch_apply repaired it; the same
  * bits as fpsketch_gated gives for that P. */
@@ -379,7 +379,8 @@ fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const voi
                                         int64_t d, int64_t f, fpsketch_dtype dtype, float* dX,
                                         float* dW, void* workspace, int64_t workspace_bytes,
                                         void* stream);
-int64_t fpsketch_gated_products_workspace(int64_t t, int64_t d, int64_t f);
+int64_t fpsketch_gated_products_workspace(const void* dP, const void* X, const void* W, int64_t t,
+                                          int64_t d, int64_t f, int32_t need_dx, int32_t need_dw);
 
 /* Low-rank adapters of many requests on a verified product C (t x n FP32) of the shared weight:
  * Y_i = C_i + scale_a (X_i A_a^T) B_a^T with a = index_i, X t x k, A count x rank x k and

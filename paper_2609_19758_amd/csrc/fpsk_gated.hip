@@ -28,6 +28,7 @@ struct MmArgs {
   const uint16_t* A;       // M x K, or K x M (K-major)
   const uint16_t* B;       // N x K, or K x N (K-major)
   int64_t M, N, K;
+  int64_t lda, ldb;        // elements from row to row as stored
   int64_t f;               // gated: N = 2f
   float* out;              // M x N (gated: may be null)
   uint16_t* H;             // gated: M x f
@@ -144,6 +145,7 @@ struct Stage {
   uint32_t rows_on;        // K-major: bytes from one load's rows to the next's
   int kk;                  // k of the first group (K-major: kRows on with each load)
 
+  // rows: of the matrix, or K-major its columns as stored (ld).
   __device__ void init(const uint16_t* x, int64_t r0, int64_t rows, int64_t ld, int64_t f) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), L = threadIdx.x;
     // gate or up rows: 16 tile rows each in turn, 8 to a wave
@@ -396,8 +398,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) 
   const Part p = part_of<BM, BN, GATED>(a);
   SA sa;
   SB sb;
-  sa.init(a.A, p.m0, a.M, AKM ? a.M : a.K, 0);
-  sb.init(a.B, p.n0, a.N, BKM ? a.N : a.K, a.f);
+  sa.init(a.A, p.m0, AKM ? a.lda : a.M, a.lda, 0);
+  sb.init(a.B, p.n0, BKM ? a.ldb : a.N, a.ldb, a.f);
   W w;
   w.init();
   auto load = [&](char* la, char* lb, int64_t k) {
@@ -462,8 +464,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_deep_kernel(MmArgs a) {
   const Part p = part_of<BM, BN, false>(a);
   SA sa;
   SB sb;
-  sa.init(a.A, p.m0, a.M, a.M, 0);
-  sb.init(a.B, p.n0, a.N, a.N, 0);
+  sa.init(a.A, p.m0, a.lda, a.lda, 0);
+  sb.init(a.B, p.n0, a.ldb, a.ldb, 0);
   W w;
   w.init();
   auto load = [&](char* la, char* lb, int64_t k) {
@@ -623,29 +625,86 @@ __global__ __launch_bounds__(kThreads) void tiny_kernel(MmArgs a, int64_t ra, in
   }
 }
 
-// The sum of the partial products in the order of the splits: one element a thread (gated: one
-// element of H, two of P).
-template <int DT, bool GATED>
+// Copies with rows padded by zeros to whole 16-byte groups, for the loads that go straight to LDS: up
+// to three matrices in one launch, a group a thread.
+struct PadArgs {
+  const uint16_t* src[3];
+  uint16_t* dst[3];
+  int64_t rows[3], cols[3];
+};
+
+__device__ __host__ inline int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+__global__ __launch_bounds__(kThreads) void pad_kernel(PadArgs a) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
+  for (int m = 0; m < 3; ++m) {
+    const int64_t groups = padded(a.cols[m]) / 8, total = a.rows[m] * a.cols[m];
+    for (int64_t o = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; o < a.rows[m] * groups; o += step) {
+      const int64_t r = o / groups, c = 8 * (o - r * groups);
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (total >= 8) {
+        v = load_ragged(a.src[m], r * a.cols[m] + c, a.cols[m] - c, total);
+      } else {
+        for (int e = 0; e < 8; ++e) {
+          if (c + e < a.cols[m]) {
+            v[e / 2] |= static_cast<uint32_t>(a.src[m][r * a.cols[m] + c + e]) << (16 * (e & 1));
+          }
+        }
+      }
+      *reinterpret_cast<u32x4*>(a.dst[m] + 8 * o) = v;
+    }
+  }
+}
+
+// The sum of the partial products in the order of the splits: V neighbours a thread (gated: of H, and
+// the same of both halves of P).  V = 4 where rows are whole groups of 4.
+template <int V>
+__device__ __forceinline__ void add_parts(const MmArgs& a, int64_t at, float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = 0.0f;
+  const int64_t size = a.M * a.N;
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    const float* p = a.part + s * size + at;
+    if constexpr (V == 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[e];
+    } else {
+      v[0] += p[0];
+    }
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void put_floats(float* to, const float (&v)[V]) {
+  if constexpr (V == 4) {
+    *reinterpret_cast<f32x4_a4*>(to) = f32x4{v[0], v[1], v[2], v[3]};
+  } else {
+    to[0] = v[0];
+  }
+}
+
+template <int DT, bool GATED, int V>
 __global__ __launch_bounds__(kThreads) void mm_sum_kernel(MmArgs a, int act) {
   const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
-  const int64_t count = a.M * (GATED ? a.f : a.N), size = a.M * a.N;
+  const int64_t cols = GATED ? a.f : a.N, count = a.M * cols / V;
   for (int64_t o = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; o < count; o += step) {
     if constexpr (GATED) {
-      const int64_t m = o / a.f, at = m * a.N + (o - m * a.f);
-      float g = 0.0f, u = 0.0f;
-      for (int s = 0; s < a.splits; ++s) {
-        g += a.part[s * size + at];
-        u += a.part[s * size + at + a.f];
-      }
+      const int64_t m = V * o / cols, at = m * a.N + (V * o - m * cols);
+      float g[V], u[V];
+      add_parts<V>(a, at, g);
+      add_parts<V>(a, at + a.f, u);
       if (a.out != nullptr) {
-        a.out[at] = g;
-        a.out[at + a.f] = u;
+        put_floats<V>(a.out + at, g);
+        put_floats<V>(a.out + at + a.f, u);
       }
-      a.H[o] = to_half<DT>(gate_up<DT>(act, g, u));
+#pragma unroll
+      for (int e = 0; e < V; ++e) a.H[V * o + e] = to_half<DT>(gate_up<DT>(act, g[e], u[e]));
     } else {
-      float v = 0.0f;
-      for (int s = 0; s < a.splits; ++s) v += a.part[s * size + o];
-      a.out[o] = v;
+      float v[V];
+      add_parts<V>(a, V * o, v);
+      put_floats<V>(a.out + V * o, v);
     }
   }
 }
@@ -777,10 +836,11 @@ struct Cut {
 };
 
 // cols: columns of the product, or of H (two of the product each).
-Cut cut_of(int64_t M, int64_t cols, bool gated, int64_t K, bool direct, int cus) {
+Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct, int cus) {
   Cut c;
   c.direct = direct;
-  c.few = gated && M <= kFew;
+  c.big = false;
+  c.few = few;
   if (c.few) {
     c.tiles_m = 1;
     c.tiles_n = (cols + 15) / 16;
@@ -808,24 +868,74 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, int64_t K, bool direct, int cus)
   return c;
 }
 
-// Operands that the loads to LDS fit: rows of whole 16-byte groups on 16-byte boundaries.
-bool direct_ok(const void* a, int64_t lda, const void* b, int64_t ldb) {
-  return lda % 8 == 0 && ldb % 8 == 0 && lda <= kMaxLd && ldb <= kMaxLd && aligned(a, 16) && aligned(b, 16);
+// An operand that the loads to LDS fit as it is: rows of whole 16-byte groups on 16-byte boundaries.
+bool fits(const void* p, int64_t ld) { return ld % 8 == 0 && aligned(p, 16); }
+
+// Whether a product is worth padded copies of the `elements` that do not fit: the copy moves 4 bytes
+// an element at 5 TB/s, the kernel for any alignment reaches half of the other's petaflop a second.
+bool worth_copies(int64_t elements, int64_t M, int64_t N, int64_t K) {
+  return 400.0 * static_cast<double>(elements) <= static_cast<double>(M) * N * K;
+}
+
+// The workspace of a call in the order it is handed out; addresses only where there is one.
+struct Space {
+  char* base;
+  int64_t used = 0;
+  void* take(int64_t bytes) {
+    void* p = base == nullptr ? nullptr : base + used;
+    used += (bytes + 15) / 16 * 16;
+    return p;
+  }
+};
+
+// An operand of a call: as it is, or its padded copy.
+struct Operand {
+  const uint16_t* p;
+  int64_t rows, cols, ld;
+  bool fit;
+};
+
+Operand operand(const void* p, int64_t rows, int64_t cols) {
+  return {static_cast<const uint16_t*>(p), rows, cols, cols, fits(p, cols)};
+}
+
+// Gives x a padded copy: its place in the workspace and its part in the launch that fills it.
+void copy_padded(Operand& x, Space& space, PadArgs& pad, int& pads) {
+  if (x.fit) return;
+  x.ld = padded(x.cols);
+  auto* to = static_cast<uint16_t*>(space.take(2 * x.rows * x.ld));
+  pad.src[pads] = x.p;
+  pad.dst[pads] = to;
+  pad.rows[pads] = x.rows;
+  pad.cols[pads] = x.cols;
+  ++pads;
+  x.p = to;
+  x.fit = true;
+}
+
+hipError_t launch_pad(const PadArgs& pad, int pads, hipStream_t st) {
+  if (pads == 0) return hipSuccess;
+  int64_t most = 0;
+  for (int m = 0; m < pads; ++m) most = std::max(most, pad.rows[m] * padded(pad.cols[m]) / 8);
+  if (most == 0) return hipSuccess;
+  const auto grid = static_cast<unsigned>(std::min<int64_t>((most + kThreads - 1) / kThreads, 8192));
+  FPSK_LAUNCH(pad_kernel, dim3(grid), dim3(kThreads), 0, st, pad);
+  return hipSuccess;
 }
 
 template <int DT, bool AKM, bool BKM, bool GATED>
 hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
-  if (a.K > 0 && (a.M * a.K < 8 || a.N * a.K < 8)) {
+  a.tiles_m = c.tiles_m;
+  a.tiles_n = c.tiles_n;
+  a.splits = c.splits;
+  a.kslice = c.kslice;
+  if (!c.direct && !c.few && a.K > 0 && (a.M * a.K < 8 || a.N * a.K < 8)) {
     const int64_t count = a.M * (GATED ? a.f : a.N);
     const auto g = static_cast<unsigned>(std::min<int64_t>((count + kThreads - 1) / kThreads, 8192));
     FPSK_LAUNCH((tiny_kernel<DT, GATED>), dim3(g), dim3(kThreads), 0, st, a, AKM ? 1 : a.K,
                 AKM ? a.M : 1, BKM ? 1 : a.K, BKM ? a.N : 1, act);
     return hipSuccess;
   }
-  a.tiles_m = c.tiles_m;
-  a.tiles_n = c.tiles_n;
-  a.splits = c.splits;
-  a.kslice = c.kslice;
   if constexpr (GATED) {
     if (c.few) {
       FPSK_LAUNCH((few_kernel<DT, 4, 2>), dim3(static_cast<unsigned>(c.tiles_n)), dim3(256), 0, st, a, act);
@@ -846,14 +956,19 @@ hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
   }
   if (c.splits > 1) {
     const int64_t count = a.M * (GATED ? a.f : a.N);
-    const auto g = static_cast<unsigned>(std::min<int64_t>((count + kThreads - 1) / kThreads, 8192));
-    FPSK_LAUNCH((mm_sum_kernel<DT, GATED>), dim3(g), dim3(kThreads), 0, st, a, act);
+    const bool four = (GATED ? a.f : a.M * a.N) % 4 == 0;
+    const auto g = static_cast<unsigned>(std::min<int64_t>((count / (four ? 4 : 1) + kThreads - 1) / kThreads, 8192));
+    if (four) {
+      FPSK_LAUNCH((mm_sum_kernel<DT, GATED, 4>), dim3(g), dim3(kThreads), 0, st, a, act);
+    } else {
+      FPSK_LAUNCH((mm_sum_kernel<DT, GATED, 1>), dim3(g), dim3(kThreads), 0, st, a, act);
+    }
   }
   return hipSuccess;
 }
 
 bool dims_ok(int64_t t, int64_t d, int64_t f) {
-  if (t < 0 || d < 1 || f < 1 || t >= kDimLimit || d >= kDimLimit || f >= kDimLimit / 2) return false;
+  if (t < 0 || d < 1 || f < 1 || t >= kDimLimit || d > kMaxLd || 2 * f > kMaxLd) return false;
   // element counts stay inside 2^40, and the tiles of a product inside one launch
   const double most = 1099511627776.0;
   const double td = static_cast<double>(t) * static_cast<double>(d);
@@ -870,6 +985,80 @@ int64_t part_bytes(const Cut& c, int64_t M, int64_t N) {
   return c.splits > 1 ? static_cast<int64_t>(c.splits) * M * N * 4 : 0;
 }
 
+// What a call of fpsketch_gated does, and the workspace it takes.
+struct GatedPlan {
+  Operand x, w;
+  PadArgs pad{};
+  int pads = 0;
+  Cut cut;
+  float* part;
+  int64_t bytes;
+};
+
+GatedPlan plan_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f, void* workspace, int cus) {
+  GatedPlan g;
+  Space space{static_cast<char*>(workspace)};
+  g.x = operand(X, t, d);
+  g.w = operand(W, 2 * f, d);
+  const bool few = t <= kFew && t * d >= 8 && 2 * f * d >= 8;
+  const int64_t odd = (g.x.fit ? 0 : t * d) + (g.w.fit ? 0 : 2 * f * d);
+  if (!few && worth_copies(odd, t, 2 * f, d)) {
+    copy_padded(g.x, space, g.pad, g.pads);
+    copy_padded(g.w, space, g.pad, g.pads);
+  }
+  g.cut = cut_of(t, f, true, few, d, g.x.fit && g.w.fit, cus);
+  g.part = static_cast<float*>(space.take(part_bytes(g.cut, t, 2 * f)));
+  g.bytes = space.used;
+  return g;
+}
+
+// The same for fpsketch_gated_products; the two products run one after the other and share the room
+// for their parts.
+struct ProductsPlan {
+  Operand p, x, w, xw;     // dP, X, W; dP as dX takes it
+  PadArgs pad{};
+  int pads = 0;
+  Cut dx, dw;
+  float* part;
+  int64_t bytes;
+};
+
+ProductsPlan plan_products(const void* dP, const void* X, const void* W, int64_t t, int64_t d, int64_t f,
+                           bool need_dx, bool need_dw, void* workspace, int cus) {
+  ProductsPlan g;
+  Space space{static_cast<char*>(workspace)};
+  g.p = operand(dP, t, 2 * f);
+  g.x = operand(X, t, d);
+  g.w = operand(W, 2 * f, d);
+  const int64_t odd_p = g.p.fit ? 0 : 2 * t * f;
+  // dP is copied once for both
+  const bool dx = need_dx && worth_copies(odd_p + (g.w.fit ? 0 : 2 * f * d), t, d, 2 * f);
+  const bool dw = need_dw && worth_copies((dx ? 0 : odd_p) + (g.x.fit ? 0 : t * d), 2 * f, d, t);
+  g.xw = g.p;
+  if (dx || dw) copy_padded(g.p, space, g.pad, g.pads);
+  if (dx) {
+    g.xw = g.p;
+    copy_padded(g.w, space, g.pad, g.pads);
+  }
+  if (dw) {
+    copy_padded(g.x, space, g.pad, g.pads);
+  } else {
+    g.p = operand(dP, t, 2 * f);
+  }
+  g.dx = cut_of(std::max<int64_t>(t, 1), d, false, false, 2 * f, g.xw.fit && g.w.fit, cus);
+  g.dw = cut_of(2 * f, d, false, false, t, g.p.fit && g.x.fit, cus);
+  int64_t part = 0;
+  if (need_dx && t > 0) part = part_bytes(g.dx, t, d);
+  if (need_dw) part = std::max(part, part_bytes(g.dw, 2 * f, d));
+  g.part = static_cast<float*>(space.take(part));
+  g.bytes = space.used;
+  return g;
+}
+
+bool workspace_ok(const void* workspace, int64_t bytes, int64_t need) {
+  return need == 0 || (workspace != nullptr && bytes >= need && aligned(workspace, 16));
+}
+
 }  // namespace
 
 }  // namespace fpsk
@@ -878,11 +1067,10 @@ using namespace fpsk;
 
 extern "C" {
 
-int64_t fpsketch_gated_workspace(int64_t t, int64_t d, int64_t f) {
+int64_t fpsketch_gated_workspace(const void* X, const void* W, int64_t t, int64_t d, int64_t f) {
   int cus = 0;
   if (!dims_ok(t, d, f) || t == 0 || layer_device(&cus) != FPSK_OK) return 0;
-  return std::max(part_bytes(cut_of(t, f, true, d, true, cus), t, 2 * f),
-                  part_bytes(cut_of(t, f, true, d, false, cus), t, 2 * f));
+  return plan_gated(X, W, t, d, f, nullptr, cus).bytes;
 }
 
 fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f,
@@ -899,29 +1087,33 @@ fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t 
   int cus = 0;
   const fpsketch_status s = layer_device(&cus);
   if (s != FPSK_OK) return s;
-  const Cut c = cut_of(t, f, true, d, direct_ok(X, d, W, d), cus);
-  const int64_t need = part_bytes(c, t, 2 * f);
-  if (!launch_fits(c)) return layer_error(FPSK_ESHAPE, "fpsketch_gated: too many tiles");
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16))) {
+  const GatedPlan g = plan_gated(X, W, t, d, f, workspace, cus);
+  if (!launch_fits(g.cut)) return layer_error(FPSK_ESHAPE, "fpsketch_gated: too many tiles");
+  if (!workspace_ok(workspace, workspace_bytes, g.bytes)) {
     return layer_error(FPSK_EINVAL, "fpsketch_gated: workspace smaller than fpsketch_gated_workspace, or not aligned to 16 bytes");
   }
   const Span in[] = {{X, 2 * t * d}, {W, 4 * f * d}};
-  const Span out[] = {{H, 2 * t * f}, {P, 8 * t * f}, {workspace, need}};
+  const Span out[] = {{H, 2 * t * f}, {P, 8 * t * f}, {workspace, g.bytes}};
   if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated: an output overlaps another argument");
   MmArgs a{};
-  a.A = static_cast<const uint16_t*>(X);
-  a.B = static_cast<const uint16_t*>(W);
+  a.A = g.x.p;
+  a.B = g.w.p;
   a.M = t;
   a.N = 2 * f;
   a.K = d;
+  a.lda = g.x.ld;
+  a.ldb = g.w.ld;
   a.f = f;
   a.out = P;
   a.H = static_cast<uint16_t*>(H);
-  a.part = static_cast<float*>(workspace);
+  a.part = g.part;
   const auto st = static_cast<hipStream_t>(stream);
-  return launched(dtype == FPSK_BF16 ? launch_mm<1, false, false, true>(a, c, act, st)
-                                     : launch_mm<0, false, false, true>(a, c, act, st),
-                  "fpsketch_gated");
+  hipError_t e = launch_pad(g.pad, g.pads, st);
+  if (e == hipSuccess) {
+    e = dtype == FPSK_BF16 ? launch_mm<1, false, false, true>(a, g.cut, act, st)
+                           : launch_mm<0, false, false, true>(a, g.cut, act, st);
+  }
+  return launched(e, "fpsketch_gated");
 }
 
 fpsketch_status fpsketch_gated_narrow(const float* P, int64_t t, int64_t f, fpsketch_dtype dtype,
@@ -979,16 +1171,11 @@ fpsketch_status fpsketch_gated_grad(const void* dH, const float* P, int64_t t, i
                   "fpsketch_gated_grad");
 }
 
-int64_t fpsketch_gated_products_workspace(int64_t t, int64_t d, int64_t f) {
+int64_t fpsketch_gated_products_workspace(const void* dP, const void* X, const void* W, int64_t t,
+                                          int64_t d, int64_t f, int32_t need_dx, int32_t need_dw) {
   int cus = 0;
   if (!dims_ok(t, d, f) || layer_device(&cus) != FPSK_OK) return 0;
-  // the two products run one after the other and share it
-  int64_t n = 0;
-  for (const bool direct : {false, true}) {
-    if (t > 0) n = std::max(n, part_bytes(cut_of(t, d, false, 2 * f, direct, cus), t, d));
-    n = std::max(n, part_bytes(cut_of(2 * f, d, false, t, direct, cus), 2 * f, d));
-  }
-  return n;
+  return plan_products(dP, X, W, t, d, f, need_dx != 0, need_dw != 0, nullptr, cus).bytes;
 }
 
 fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const void* W, int64_t t,
@@ -997,7 +1184,7 @@ fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const voi
                                         void* stream) {
   if (!half_type(dtype)) return layer_error(FPSK_EDTYPE, "fpsketch_gated_products: dP, X and W are FP16 or BF16");
   if (!dims_ok(t, d, f)) return layer_error(FPSK_ESHAPE, "fpsketch_gated_products: dimensions");
-  if (dX == nullptr && dW == nullptr) return layer_error(FPSK_EINVAL, "fpsketch_gated_products: no output");
+  if (dX == nullptr && dW == nullptr && t > 0) return layer_error(FPSK_EINVAL, "fpsketch_gated_products: no output");
   if ((t > 0 && dP == nullptr) || (t > 0 && dW != nullptr && X == nullptr) ||
       (t > 0 && dX != nullptr && W == nullptr)) {
     return layer_error(FPSK_EINVAL, "fpsketch_gated_products: null pointer");
@@ -1008,41 +1195,44 @@ fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const voi
   int cus = 0;
   const fpsketch_status s = layer_device(&cus);
   if (s != FPSK_OK) return s;
-  const Cut cx = cut_of(std::max<int64_t>(t, 1), d, false, 2 * f, direct_ok(dP, 2 * f, W, d), cus);
-  const Cut cw = cut_of(2 * f, d, false, t, direct_ok(dP, 2 * f, X, d), cus);
-  int64_t need = 0;
-  if (dX != nullptr && t > 0) need = part_bytes(cx, t, d);
-  if (dW != nullptr) need = std::max(need, part_bytes(cw, 2 * f, d));
-  if (!launch_fits(cx) || !launch_fits(cw)) return layer_error(FPSK_ESHAPE, "fpsketch_gated_products: too many tiles");
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16))) {
+  const bool need_dx = dX != nullptr, need_dw = dW != nullptr;
+  const ProductsPlan g = plan_products(dP, X, W, t, d, f, need_dx, need_dw, workspace, cus);
+  if ((need_dx && !launch_fits(g.dx)) || (need_dw && !launch_fits(g.dw))) {
+    return layer_error(FPSK_ESHAPE, "fpsketch_gated_products: too many tiles");
+  }
+  if (!workspace_ok(workspace, workspace_bytes, g.bytes)) {
     return layer_error(FPSK_EINVAL, "fpsketch_gated_products: workspace smaller than fpsketch_gated_products_workspace, or not aligned to 16 bytes");
   }
   const Span in[] = {{dP, 4 * t * f}, {X, 2 * t * d}, {W, 4 * f * d}};
-  const Span out[] = {{dX, 4 * t * d}, {dW, 8 * f * d}, {workspace, need}};
+  const Span out[] = {{dX, 4 * t * d}, {dW, 8 * f * d}, {workspace, g.bytes}};
   if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated_products: an output overlaps another argument");
   const auto st = static_cast<hipStream_t>(stream);
-  hipError_t e = hipSuccess;
+  hipError_t e = launch_pad(g.pad, g.pads, st);
   MmArgs a{};
-  a.part = static_cast<float*>(workspace);
-  if (dX != nullptr && t > 0) {
-    a.A = static_cast<const uint16_t*>(dP);
-    a.B = static_cast<const uint16_t*>(W);
+  a.part = g.part;
+  if (e == hipSuccess && need_dx && t > 0) {
+    a.A = g.xw.p;
+    a.B = g.w.p;
     a.M = t;
     a.N = d;
     a.K = 2 * f;
+    a.lda = g.xw.ld;
+    a.ldb = g.w.ld;
     a.out = dX;
-    e = dtype == FPSK_BF16 ? launch_mm<1, false, true, false>(a, cx, 0, st)
-                           : launch_mm<0, false, true, false>(a, cx, 0, st);
+    e = dtype == FPSK_BF16 ? launch_mm<1, false, true, false>(a, g.dx, 0, st)
+                           : launch_mm<0, false, true, false>(a, g.dx, 0, st);
   }
-  if (e == hipSuccess && dW != nullptr) {
-    a.A = static_cast<const uint16_t*>(dP);
-    a.B = static_cast<const uint16_t*>(X);
+  if (e == hipSuccess && need_dw) {
+    a.A = g.p.p;
+    a.B = g.x.p;
     a.M = 2 * f;
     a.N = d;
     a.K = t;
+    a.lda = g.p.ld;
+    a.ldb = g.x.ld;
     a.out = dW;
-    e = dtype == FPSK_BF16 ? launch_mm<1, true, true, false>(a, cw, 0, st)
-                           : launch_mm<0, true, true, false>(a, cw, 0, st);
+    e = dtype == FPSK_BF16 ? launch_mm<1, true, true, false>(a, g.dw, 0, st)
+                           : launch_mm<0, true, true, false>(a, g.dw, 0, st);
   }
   return launched(e, "fpsketch_gated_products");
 }

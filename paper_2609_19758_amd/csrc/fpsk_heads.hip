@@ -380,18 +380,20 @@ __global__ __launch_bounds__(kThreads) void heads_grad_kernel(HeadArgs a) {
   }
 }
 
-// The gains' gradients: the work-groups' sums, one entry per wave.
-__global__ __launch_bounds__(64) void gains_kernel(HeadArgs a) {
-  const int e = blockIdx.x, lane = threadIdx.x;
+// The gains' gradients: the work-groups' sums, one entry per work-group.
+__global__ __launch_bounds__(kThreads) void gains_kernel(HeadArgs a) {
+  __shared__ double sums[kThreads / 64];
+  const float* p = a.part + static_cast<int64_t>(blockIdx.x) * a.groups;
   double s = 0.0;
-  for (int g = lane; g < a.groups; g += 64) s += a.part[static_cast<int64_t>(e) * a.groups + g];
+#pragma unroll 4
+  for (int g = threadIdx.x; g < a.groups; g += kThreads) s += p[g];
+#pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (lane == 0) {
-    if (e < a.hd) {
-      a.dgq[e] = static_cast<float>(s);
-    } else {
-      a.dgk[e - a.hd] = static_cast<float>(s);
-    }
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int e = blockIdx.x;
+    (e < a.hd ? a.dgq[e] : a.dgk[e - a.hd]) = static_cast<float>((sums[0] + sums[1]) + (sums[2] + sums[3]));
   }
 }
 
@@ -577,7 +579,7 @@ fpsketch_status fpsketch_heads_grad(const void* dq, const void* dk, const void* 
     e = dtype == FPSK_BF16 ? launch_heads<1>(a, true, vec, grid, st) : launch_heads<0>(a, true, vec, grid, st);
   }
   if (e == hipSuccess && norm) {
-    e = launch_k(gains_kernel, dim3(static_cast<unsigned>(2 * hd)), dim3(64), 0, st, nullptr, nullptr, a);
+    e = launch_k(gains_kernel, dim3(static_cast<unsigned>(2 * hd)), dim3(kThreads), 0, st, nullptr, nullptr, a);
   }
   return launched(e, "fpsketch_heads_grad");
 }

@@ -102,13 +102,13 @@ _SIGS = {
     # operators around a delivered product (layers.py)
     "fpsketch_gated": (ctypes.c_int, [_P, _P, _I64, _I64, _I64, ctypes.c_int, ctypes.c_int, _P, _P,
                                       _P, _I64, _P]),
-    "fpsketch_gated_workspace": (_I64, [_I64, _I64, _I64]),
+    "fpsketch_gated_workspace": (_I64, [_P, _P, _I64, _I64, _I64]),
     "fpsketch_gated_narrow": (ctypes.c_int, [_P, _I64, _I64, ctypes.c_int, ctypes.c_int, _P, _P]),
     "fpsketch_gated_grad": (ctypes.c_int, [_P, _P, _I64, _I64, ctypes.c_int, ctypes.c_int, _P, _P,
                                            _P]),
     "fpsketch_gated_products": (ctypes.c_int, [_P, _P, _P, _I64, _I64, _I64, ctypes.c_int, _P, _P,
                                                _P, _I64, _P]),
-    "fpsketch_gated_products_workspace": (_I64, [_I64, _I64, _I64]),
+    "fpsketch_gated_products_workspace": (_I64, [_P, _P, _P, _I64, _I64, _I64, _I32, _I32]),
     "fpsketch_adapters": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I32, _I32,
                                          ctypes.c_int, _P, ctypes.c_int, _P, _I64, _P]),
     "fpsketch_adapters_workspace": (_I64, [_I64, _I64, _I64, _I32, _I32]),

@@ -129,7 +129,7 @@ def gated(X, W, act: str = "silu", deliver: bool = True, H=None, P=None, stream=
         pp = 0
         if deliver:
             P, pp = c.output(P, "P", (t, rows), _F32)
-        n = lib.fpsketch_gated_workspace(t, d, f)
+        n = lib.fpsketch_gated_workspace(x, w, t, d, f)
         ws, wp = c.workspace(n)
         fk._check(lib.fpsketch_gated(x, w, t, d, f, code, a, hp, pp, wp, n, c.stream),
                   "fpsketch_gated")
@@ -200,7 +200,7 @@ def gated_products(dP, X, W, need_dx: bool = True, need_dw: bool = True, dX=None
             dX, xp = c.output(dX, "dX", (t, d), _F32)
         if need_dw:
             dW, gp = c.output(dW, "dW", (rows, d), _F32)
-        n = lib.fpsketch_gated_products_workspace(t, d, f)
+        n = lib.fpsketch_gated_products_workspace(p, x, w, t, d, f, need_dx, need_dw)
         ws, wp = c.workspace(n)
         fk._check(lib.fpsketch_gated_products(p, x, w, t, d, f, code, xp, gp, wp, n, c.stream),
                   "fpsketch_gated_products")
