@@ -224,14 +224,14 @@ __device__ __forceinline__ void store4h(uint16_t* row, int64_t j, int64_t n, u16
 
 // Work-groups are dealt to the 8 XCDs in turn; each XCD gets neighbouring tiles, in bands of 8 rows
 // of tiles, so that its L2 holds the operands' tiles that they share.
-__device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn, int64_t* m, int64_t* n) {
-  const int64_t count = tm * tn, per = count / 8;
+__device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
+  const uint32_t per = tm * tn / 8;
   if (b < 8 * per) b = (b % 8) * per + b / 8;
-  const int64_t band = b / (8 * tn), first = 8 * band;
-  const int64_t height = tm - first < 8 ? tm - first : 8;
-  const int64_t in = b - band * 8 * tn;
-  *m = first + in % height;
+  const uint32_t band = b / (8 * tn), first = 8 * band;
+  const uint32_t height = tm - first < 8 ? tm - first : 8;
+  const uint32_t in = b - band * 8 * tn;
   *n = in / height;
+  *m = first + in - *n * height;
 }
 
 // Accumulators of a wave: BM / WM x BN / WN of the tile.
@@ -267,6 +267,28 @@ struct Wave {
 #pragma unroll
         for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[j], fa, acc[i][j]);
       }
+    }
+  }
+
+  // The same with a row block's fragment read two blocks ahead of its products, and the second half's
+  // fragments of B during the last blocks of the first; the barriers keep the scheduler from moving
+  // the reads down to their use, where the matrix cores would wait for LDS (796 -> 747 us at 4096 x
+  // 4096 x 22016).
+  __device__ __forceinline__ void multiply_ahead(const char* la, const char* lb) {
+    static_assert(MT >= NTL && MT > 2, "");
+    u32x4 fa[3], fb[2][NTL];
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) fb[0][j] = TB::frag(lb, wn + 16 * j, 0);
+    fa[0] = TA::frag(la, wm, 0);
+    fa[1] = TA::frag(la, wm + 16, 0);
+#pragma unroll
+    for (int g = 0; g < 2 * MT; ++g) {
+      const int ks = g / MT, i = g % MT, next = g + 2;
+      if (next < 2 * MT) fa[next % 3] = TA::frag(la, wm + 16 * (next % MT), next / MT);
+      if (ks == 0 && i >= MT - NTL) fb[1][i - (MT - NTL)] = TB::frag(lb, wn + 16 * (i - (MT - NTL)), 1);
+#pragma unroll
+      for (int j = 0; j < NTL; ++j) acc[i][j] = mfma32<DT>(fb[ks][j], fa[g % 3], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -314,13 +336,15 @@ struct Part {
 
 template <int BM, int BN, bool GATED>
 __device__ __forceinline__ Part part_of(const MmArgs& a) {
-  const int64_t tiles = a.tiles_m * a.tiles_n;
+  // (32 bits: a launch has fewer work-groups, and a 64-bit division takes a microsecond)
+  const auto rows = static_cast<uint32_t>(a.tiles_m), cols = static_cast<uint32_t>(a.tiles_n);
+  const uint32_t split = blockIdx.x / (rows * cols);
+  uint32_t tm, tn;
+  tile_of(blockIdx.x - split * rows * cols, rows, cols, &tm, &tn);
   Part p;
-  int64_t tm, tn;
-  p.split = blockIdx.x / tiles;
-  tile_of(blockIdx.x - p.split * tiles, a.tiles_m, a.tiles_n, &tm, &tn);
-  p.m0 = tm * BM;
-  p.n0 = tn * (GATED ? BN / 2 : BN);
+  p.split = split;
+  p.m0 = static_cast<int64_t>(tm) * BM;
+  p.n0 = static_cast<int64_t>(tn) * (GATED ? BN / 2 : BN);
   p.k0 = p.split * a.kslice;
   p.k1 = p.k0 + a.kslice < a.K ? p.k0 + a.kslice : a.K;
   return p;
@@ -379,18 +403,13 @@ __device__ __forceinline__ void stages_ready() {
 }
 
 // Whole 16-byte groups, two buffers of 64 k: the next step's loads are under way during this one's
-// products.  A row block's fragment is read two blocks ahead of its products, the second half's
-// fragments of B during the last blocks of the first; the barriers keep the scheduler from moving
-// the reads down to their use, where the matrix cores would wait for LDS (796 -> 747 us at 4096 x
-// 4096 x 22016).  A buffer is an array of its own, so that the compiler knows loads into one apart
-// from reads of the other.
+// products.  A buffer is an array of its own, so that the compiler knows loads into one apart from
+// reads of the other.
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) {
   typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
   typedef Stage<BM, W::NT, kBK, AKM, false> SA;
   typedef Stage<BN, W::NT, kBK, BKM, GATED> SB;
-  constexpr int MT = W::MT, NTL = W::NTL;
-  static_assert(MT >= NTL && MT > 2, "");
   __shared__ __attribute__((aligned(16))) char a0[SA::kBytes];
   __shared__ __attribute__((aligned(16))) char b0[SB::kBytes];
   __shared__ __attribute__((aligned(16))) char a1[SA::kBytes];
@@ -407,34 +426,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) 
     sb.load(lb, k, p.k1);
     __builtin_amdgcn_sched_barrier(0);     // (else the loads sink to the end of the products)
   };
-  auto multiply = [&](const char* la, const char* lb) {
-    u32x4 fa[3], fb[2][NTL];
-#pragma unroll
-    for (int j = 0; j < NTL; ++j) fb[0][j] = W::TB::frag(lb, w.wn + 16 * j, 0);
-    fa[0] = W::TA::frag(la, w.wm, 0);
-    fa[1] = W::TA::frag(la, w.wm + 16, 0);
-#pragma unroll
-    for (int g = 0; g < 2 * MT; ++g) {
-      const int ks = g / MT, i = g % MT, next = g + 2;
-      if (next < 2 * MT) fa[next % 3] = W::TA::frag(la, w.wm + 16 * (next % MT), next / MT);
-      if (ks == 0 && i >= MT - NTL) fb[1][i - (MT - NTL)] = W::TB::frag(lb, w.wn + 16 * (i - (MT - NTL)), 1);
-#pragma unroll
-      for (int j = 0; j < NTL; ++j) w.acc[i][j] = mfma32<DT>(fb[ks][j], fa[g % 3], w.acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
   load(a0, b0, p.k0);
   int64_t k = p.k0;
   for (; k + kBK < p.k1; k += 2 * kBK) {   // (loads past K fill a buffer with zeros)
     stages_ready<0>();
     load(a1, b1, k + kBK);
-    multiply(a0, b0);
+    w.multiply_ahead(a0, b0);
     stages_ready<0>();
     load(a0, b0, k + 2 * kBK);
-    multiply(a1, b1);
+    w.multiply_ahead(a1, b1);
   }
   stages_ready<0>();                       // no load outlives the kernel
-  if (k < p.k1) multiply(a0, b0);
+  if (k < p.k1) w.multiply_ahead(a0, b0);
   w.store(a, p.m0, p.n0, p.split, act);
 }
 
@@ -871,10 +874,12 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct
 // An operand that the loads to LDS fit as it is: rows of whole 16-byte groups on 16-byte boundaries.
 bool fits(const void* p, int64_t ld) { return ld % 8 == 0 && aligned(p, 16); }
 
-// Whether a product is worth padded copies of the `elements` that do not fit: the copy moves 4 bytes
-// an element at 5 TB/s, the kernel for any alignment reaches half of the other's petaflop a second.
+// Whether a product is worth padded copies of the `elements` that do not fit: small ones, whose copy is
+// one short launch (gated 400 x 1023 x 1000: 21 us, 29 us with the kernel for any alignment), and
+// those with the work to make up for it (4095 x 4096: 63 against 91 us at 300 tokens, but 58 against
+// 52 us at 130 and 42 against 29 us at 20).
 bool worth_copies(int64_t elements, int64_t M, int64_t N, int64_t K) {
-  return 400.0 * static_cast<double>(elements) <= static_cast<double>(M) * N * K;
+  return elements <= int64_t{1} << 22 || 256.0 * static_cast<double>(elements) <= static_cast<double>(M) * N * K;
 }
 
 // The workspace of a call in the order it is handed out; addresses only where there is one.
