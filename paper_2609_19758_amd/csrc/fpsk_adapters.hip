@@ -23,7 +23,8 @@ struct AdapterArgs {
   const float* scale;
   int64_t t, k, n;
   int count, rank;
-  float* V;                // splits x t x rank: partial sums of X_i A_a^T
+  float* V;                // splits x t x ldv: partial sums of X_i A_a^T (ldv: rank in whole groups of 4)
+  int ldv;
   void* Y;
   int64_t tiles;
   int ways;                // work-groups that share a tile's adapters
@@ -32,8 +33,7 @@ struct AdapterArgs {
   int64_t cols;            // columns per column block
 };
 
-// Both kernels take tiles of neighbouring rows as they come, in two or three steps over the
-// adapters that a tile's rows name: an adapter's factor multiplies the whole tile on the matrix
+// Both kernels take tiles of neighbouring rows as they come, in turn over the adapters that a tile's rows name: an adapter's factor multiplies the whole tile on the matrix
 // cores, and only its own rows are kept.  The rows of a request are neighbours, so a prompt's tile
 // names one adapter or two and no sorting of rows is needed before; a decode tile names up to 16,
 // which `ways` work-groups take in turn.
@@ -57,27 +57,100 @@ __device__ __forceinline__ void for_adapters(const AdapterArgs& a, int64_t row0,
 constexpr int kShrinkWaves = 4;
 constexpr int kMaxSplits = 8;
 
-// V = X A^T: a tile of 16 MT rows, a block of 16 NT ranks and a part of k per work-group.  Bound by
-// reading X once (the factors stay in L2); fragments come straight from memory, a wave's 64 k per
-// step as 32 bytes a lane, so that the four lanes of a row read a whole 128-byte line, with the next
-// step's loads in flight during the products.  The waves take the steps in turn and their sums
-// meet in LDS; parts of k are added by the next kernel, in order.
+// What both forms of the first product do with a work-group: a tile of 16 MT rows, a block of 16 NT
+// ranks and a part of k; within it every wave a run of k.
+struct ShrinkPart {
+  int split, r0, way;
+  int64_t row0;
+};
+
+template <int TR, int RB>
+__device__ __forceinline__ ShrinkPart shrink_part(const AdapterArgs& a) {
+  ShrinkPart p;
+  unsigned b = blockIdx.x;
+  p.split = b % a.splits;
+  b /= a.splits;
+  p.r0 = b % a.blocks * RB;
+  b /= a.blocks;
+  const auto tiles = static_cast<unsigned>(a.tiles);
+  p.row0 = static_cast<int64_t>(b % tiles) * TR;
+  p.way = static_cast<int>(b / tiles);     // last: most tiles name one adapter only
+  return p;
+}
+
+// The waves' sums to V, rows of the adapter only.
+template <int TR, int RB>
+__device__ __forceinline__ void shrink_store(const AdapterArgs& a, const ShrinkPart& p, uint64_t mask,
+                                             float (*red)[TR][RB + 4]) {
+  for (int e = threadIdx.x; e < TR * RB; e += 64 * kShrinkWaves) {
+    const int r = e / RB, c = e % RB;
+    if (((mask >> r) & 1) != 0 && p.r0 + c < a.rank) {
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kShrinkWaves; ++w) v += red[w][r][c];
+      a.V[(static_cast<int64_t>(p.split) * a.t + p.row0 + r) * a.ldv + p.r0 + c] = v;
+    }
+  }
+}
+
+// V = X A^T, both streamed through LDS; the parts of k are added by the next kernel, in order.
 template <int DT, int MT, int NT>
 __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a) {
+  constexpr int TR = 16 * MT, RB = 16 * NT, kBytes = WaveRows<MT>::kBytes + WaveRows<NT>::kBytes;
+  __shared__ __attribute__((aligned(16))) char b0[kShrinkWaves * kBytes];
+  __shared__ __attribute__((aligned(16))) char b1[kShrinkWaves * kBytes];
+  __shared__ __attribute__((aligned(16))) char b2[kShrinkWaves * kBytes];
+  static_assert(sizeof(float) * kShrinkWaves * TR * (RB + 4) <= sizeof(b0) + sizeof(b1), "");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
+  const ShrinkPart p = shrink_part<TR, RB>(a);
+  const int64_t steps = (a.k + kStreamK - 1) / kStreamK, parts = static_cast<int64_t>(kShrinkWaves) * a.splits;
+  const int64_t run = (steps + parts - 1) / parts * kStreamK, k0 = (p.split * kShrinkWaves + wave) * run;
+  const int64_t k1 = k0 + run < a.k ? k0 + run : a.k;
+  for_adapters<TR>(a, p.row0, p.way, [&](int which, uint64_t mask) {
+    if (which < 0 || which >= a.count) return;
+    WaveRows<MT> x;
+    WaveRows<NT> f;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x.set(i, a.X, p.row0 + 16 * i, a.t, a.k);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      f.set(j, a.A + static_cast<int64_t>(which) * a.rank * a.k, p.r0 + 16 * j, a.rank, a.k);
+    }
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __syncthreads();                       // the sums of the adapter before
+    wave_product<DT, MT, NT>(x, f, b0 + wave * kBytes, b1 + wave * kBytes, b2 + wave * kBytes, k0, k1, acc);
+    __syncthreads();
+    auto red = reinterpret_cast<float(*)[TR][RB + 4]>(b0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        *reinterpret_cast<f32x4*>(&red[wave][16 * i + (lane & 15)][16 * j + 4 * g]) = acc[i][j];
+      }
+    }
+    __syncthreads();
+    shrink_store<TR, RB>(a, p, mask, red);
+  });
+}
+
+// The same for any alignment: fragments straight from memory, a wave's 64 k per step as 32 bytes a lane,
+// with the next step's loads in flight during the products.
+template <int DT, int MT, int NT>
+__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_ragged_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, RB = 16 * NT;
   __shared__ __attribute__((aligned(16))) float red[kShrinkWaves][TR][RB + 4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
-  unsigned b = blockIdx.x;
-  const int split = b % a.splits;
-  b /= a.splits;
-  const int rb = b % a.blocks;
-  b /= a.blocks;
-  const int64_t row0 = static_cast<int64_t>(b % a.tiles) * TR;
-  const int way = static_cast<int>(b / a.tiles);   // last: most tiles name one adapter only
-  const int r0 = rb * RB;
+  const ShrinkPart p = shrink_part<TR, RB>(a);
+  const int64_t row0 = p.row0;
+  const int r0 = p.r0, split = p.split;
   const int64_t steps = a.k / 64;                  // whole ones
 
-  for_adapters<TR>(a, row0, way, [&](int which, uint64_t mask) {
+  for_adapters<TR>(a, row0, p.way, [&](int which, uint64_t mask) {
     if (which < 0 || which >= a.count) return;
     // rows and ranks past the end repeat the last one; their sums are not stored
     int64_t xo[MT], ao[NT];
@@ -123,22 +196,21 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a
     };
     // Unconditional loads: behind a branch the compiler waits for the step ahead too.  A wave past
     // its last step reads that one again.
-    const int64_t stride = kShrinkWaves * a.splits;
-    const int64_t first = split * kShrinkWaves + __builtin_amdgcn_readfirstlane(wave);
-    const int64_t mine = first < steps ? (steps - first - 1) / stride + 1 : 0;
-    if (mine > 0) {
-      const int64_t end = first + (mine - 1) * stride;
-      fetch(0, first);
-      int64_t s = first;
-      for (int64_t left = mine; left > 1; left -= 2, s += 2 * stride) {
-        fetch(1, s + stride);
+    const int64_t turn = split * kShrinkWaves + __builtin_amdgcn_readfirstlane(wave);
+    const int64_t parts = static_cast<int64_t>(kShrinkWaves) * a.splits, run = (steps + parts - 1) / parts;
+    int64_t s = turn * run < steps ? turn * run : steps, left = steps - s < run ? steps - s : run;
+    if (left > 0) {
+      const int64_t last = s + left - 1;
+      fetch(0, s);
+      for (; left > 1; left -= 2, s += 2) {
+        fetch(1, s + 1);
         multiply(0);
-        fetch(0, s + 2 * stride < end ? s + 2 * stride : end);
+        fetch(0, s + 2 < last ? s + 2 : last);
         multiply(1);
       }
-      if (mine & 1) multiply(0);
+      if (left == 1) multiply(0);
     }
-    if (first + mine * stride == steps && 64 * steps < a.k) {  // the wave whose turn the broken last step is
+    if (turn == parts - 1 && 64 * steps < a.k) {  // the broken last step
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int64_t k0 = 64 * steps + 8 * h, nv = a.k - k0 - 16 * g;
@@ -161,15 +233,7 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a
       }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < TR * RB; e += 64 * kShrinkWaves) {
-      const int r = e / RB, c = e % RB;
-      if (((mask >> r) & 1) != 0 && r0 + c < a.rank) {
-        float v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kShrinkWaves; ++w) v += red[w][r][c];
-        a.V[(static_cast<int64_t>(split) * a.t + row0 + r) * a.rank + r0 + c] = v;
-      }
-    }
+    shrink_store<TR, RB>(a, p, mask, red);
   });
 }
 
@@ -207,20 +271,27 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
       __syncthreads();                     // the V of the adapter before
       const int r = threadIdx.x / PER, p = threadIdx.x % PER;
       const bool own = ((mask >> r) & 1) != 0;
-      const float* v = a.V + (own ? row0 + r : row0) * a.rank;
-      const int64_t part = a.t * a.rank;
+      const float* v = a.V + (own ? row0 + r : row0) * a.ldv;
+      const int64_t part = a.t * a.ldv;
       float top = 0.0f;
-      for (int c = p; c < rp; c += PER) {
-        float s = 0.0f;
-        if (own && c < a.rank) {
-          float w[kMaxSplits];             // all loads in flight, then the sum in order
+#pragma unroll 2
+      for (int c = 4 * p; c < rp; c += 4 * PER) {
+        f32x4 w[kMaxSplits];               // all loads in flight, then the sum in order
 #pragma unroll
-          for (int q = 0; q < kMaxSplits; ++q) w[q] = v[(q < a.splits ? q * part : 0) + c];
-#pragma unroll
-          for (int q = 0; q < kMaxSplits; ++q) s += q < a.splits ? w[q] : 0.0f;
+        for (int q = 0; q < kMaxSplits; ++q) {
+          w[q] = *reinterpret_cast<const f32x4*>(v + (q < a.splits ? q * part : 0) + (c < a.ldv ? c : 0));
         }
-        sums[r * rp + c] = s;
-        top = fmaxf(top, fabsf(s));
+        f32x4 sum = w[0];
+#pragma unroll
+        for (int q = 1; q < kMaxSplits; ++q) {
+          if (q < a.splits) sum += w[q];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!own || c + e >= a.rank) sum[e] = 0.0f;
+          top = fmaxf(top, fabsf(sum[e]));
+        }
+        *reinterpret_cast<f32x4*>(sums + r * rp + c) = sum;
       }
       float up = 1.0f, down = 1.0f;
       if constexpr (DT == 0) {
@@ -233,12 +304,17 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
           down = ldexpf(1.0f, e);
         }
       }
-      for (int c = p; c < rp; c += PER) {
-        const float s = sums[r * rp + c] * up;
-        const uint16_t h = to_half<DT>(s);
-        const float rest = s - from_half<DT>(h);
-        hi[r * ld + c] = h;
-        lo[r * ld + c] = fabsf(s) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
+      for (int c = 4 * p; c < rp; c += 4 * PER) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(sums + r * rp + c) * up;
+        u16x4 h, l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          h[e] = to_half<DT>(s[e]);
+          const float rest = s[e] - from_half<DT>(h[e]);
+          l[e] = fabsf(s[e]) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
+        }
+        *reinterpret_cast<u16x4*>(hi + r * ld + c) = h;
+        *reinterpret_cast<u16x4*>(lo + r * ld + c) = l;
       }
       if (p == 0) back[r] = down;
       __syncthreads();
@@ -246,8 +322,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
       for (int i = 0; i < MT; ++i) scale[i] = a.scale[which] * back[16 * i + (lane & 15)];
     }
 
-    // FULL: the wave's columns all lie in the row; C is then loaded without a branch (rows of other
-    // adapters too: they are not stored here).
+    // FULL: the wave's columns all lie in the row.
     auto columns = [&](int64_t n0, auto full) {
       constexpr bool FULL = decltype(full)::value;
       u32x4 f[NC][2];
@@ -278,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
 #pragma unroll
         for (int q = 0; q < NC; ++q) {
           const int64_t col = n0 + 32 * q + 8 * g;
-          if constexpr (FULL) {
+          if constexpr (FULL) {            // (rows of other adapters too: they are not stored here)
             y[i][q][0] = *reinterpret_cast<const f32x4_a4*>(c + col);
             y[i][q][1] = *reinterpret_cast<const f32x4_a4*>(c + col + 4);
           } else {
@@ -407,45 +482,72 @@ __global__ __launch_bounds__(kThreads) void tiny_kernel(AdapterArgs a, int half)
 
 // ---- host ------------------------------------------------------------------------------------
 
-// How the work is cut.  Long batches take 32 rows a tile (each factor is then read from L2 half as
-// often), short ones 16.  k is split in up to 8 parts, part p on XCD p (work-groups are dealt to the
-// XCDs in turn), so that an XCD's L2 holds its part of the factors for all tiles; not where the
-// partial sums would be more than half of X, unless compute units would have no work-group.
+// How the work is cut: tiles of 32 rows in long batches (each factor is then read from L2 half as
+// often), of 16 in short ones; k in up to 8 parts while the tiles do not give every compute unit two
+// work-groups; and as many work-groups to a tile's adapters as that leaves room for.
 struct Cut {
-  int mt;
+  int mt, ways;
   int64_t tiles;
-  int ways, splits, nt, rank_blocks;
 };
 
-Cut cut_of(int64_t t, int64_t k, int count, int rank, int cus) {
-  Cut c;
-  c.mt = t > 1024 ? 2 : 1;
-  const int tr = 16 * c.mt;
-  c.tiles = (t + tr - 1) / tr;
-  c.nt = rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8;
-  c.rank_blocks = (rank + 16 * c.nt - 1) / (16 * c.nt);
-  const int64_t most = std::min<int64_t>(tr, int64_t{count} + 2);
-  c.ways = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 256 / c.tiles)));
-  const int64_t steps = (k + 63) / 64, groups = c.tiles * c.rank_blocks;
-  const int64_t worth = std::max<int64_t>(k / (8 * int64_t{rank}), cus / groups);
-  c.splits = static_cast<int>(
-      std::max<int64_t>(1, std::min<int64_t>({worth, steps / kShrinkWaves, int64_t{kMaxSplits}})));
-  return c;
+struct Plan {
+  Cut shrink, expand;
+  int splits, nt, rank_blocks, ldv;
+  bool direct;
+};
+
+Cut tiles_of(int64_t t, int mt) {
+  const int tr = 16 * mt;
+  return {mt, 1, (t + tr - 1) / tr};
+}
+
+// Work-groups to a tile's adapters, where there are `groups` with one each.
+int ways_of(int mt, int64_t groups, int count, int cus) {
+  const int64_t most = std::min<int64_t>(16 * mt, int64_t{count} + 2);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, 2 * cus / groups)));
+}
+
+Plan plan_of(int64_t t, int64_t k, int count, int rank, bool direct, int cus) {
+  Plan p;
+  p.direct = direct;
+  p.nt = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
+  p.rank_blocks = (rank + 16 * p.nt - 1) / (16 * p.nt);
+  p.ldv = (rank + 3) / 4 * 4;
+  p.shrink = tiles_of(t, t > 1024 ? 2 : 1);
+  p.expand = tiles_of(t, t > 1024 ? 2 : 1);
+  const int64_t steps = (k + 63) / 64, groups = p.shrink.tiles * p.rank_blocks;
+  p.splits = static_cast<int>(
+      std::max<int64_t>(1, std::min<int64_t>({2 * cus / groups, steps / kShrinkWaves, int64_t{kMaxSplits}})));
+  p.shrink.ways = ways_of(p.shrink.mt, groups * p.splits, count, cus);
+  return p;
+}
+
+int64_t space_of(const Plan& p, int64_t t) { return int64_t{4} * p.splits * t * p.ldv; }
+
+template <int DT, int MT, int NT>
+hipError_t launch_shrink(const AdapterArgs& a, bool direct, hipStream_t st) {
+  const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks * a.splits)), block(64 * kShrinkWaves);
+  if (direct) {
+    FPSK_LAUNCH((shrink_kernel<DT, MT, NT>), grid, block, 0, st, a);
+  } else {
+    FPSK_LAUNCH((shrink_ragged_kernel<DT, MT, NT>), grid, block, 0, st, a);
+  }
+  return hipSuccess;
 }
 
 template <int DT, int MT>
-hipError_t launch_shrink(const AdapterArgs& a, int nt, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks * a.splits)), block(64 * kShrinkWaves);
-  if (nt == 1) FPSK_LAUNCH((shrink_kernel<DT, MT, 1>), grid, block, 0, st, a);
-  if (nt == 2) FPSK_LAUNCH((shrink_kernel<DT, MT, 2>), grid, block, 0, st, a);
-  if (nt == 4) FPSK_LAUNCH((shrink_kernel<DT, MT, 4>), grid, block, 0, st, a);
-  if (nt == 8) FPSK_LAUNCH((shrink_kernel<DT, MT, 8>), grid, block, 0, st, a);
-  return hipSuccess;
+hipError_t launch_shrink(AdapterArgs a, const Plan& p, hipStream_t st) {
+  a.tiles = p.shrink.tiles;
+  a.ways = p.shrink.ways;
+  a.blocks = p.rank_blocks;
+  if (p.nt == 1) return launch_shrink<DT, MT, 1>(a, p.direct, st);
+  if (p.nt == 2) return launch_shrink<DT, MT, 2>(a, p.direct, st);
+  return launch_shrink<DT, MT, 4>(a, p.direct, st);
 }
 
 template <int DT, int MT, bool HALF, bool WHOLE>
 hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
-  constexpr int NC = MT;
+  constexpr int NC = 1;
   const auto kernel = expand_kernel<DT, MT, NC, HALF, WHOLE>;
   // a work-group forms the tile's V once for all its columns: as many as leave three work-groups for
   // every compute unit
@@ -453,6 +555,7 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
   const int64_t each = std::max<int64_t>(1, std::min<int64_t>(steps, a.tiles * steps / (3 * cus)));
   a.cols = each * 128 * NC;
   a.blocks = static_cast<int>((a.n + a.cols - 1) / a.cols);
+  a.ways = ways_of(MT, a.tiles * a.blocks, a.count, 4 * cus);
   const int rp = (a.rank + 31) / 32 * 32;
   const size_t lds = static_cast<size_t>(16 * MT) * (4 * (rp + 8) + 4 * rp + 4);
   const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks)), block(kThreads);
@@ -466,13 +569,10 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
 }
 
 template <int DT, int MT>
-hipError_t launch_adapters(AdapterArgs a, const Cut& c, bool half, int cus, hipStream_t st) {
-  a.tiles = c.tiles;
-  a.ways = c.ways;
-  a.splits = c.splits;
-  a.blocks = c.rank_blocks;
-  const hipError_t e = launch_shrink<DT, MT>(a, c.nt, st);
+hipError_t launch_adapters(AdapterArgs a, const Plan& p, bool half, int cus, hipStream_t st) {
+  const hipError_t e = p.shrink.mt == 2 ? launch_shrink<DT, 2>(a, p, st) : launch_shrink<DT, 1>(a, p, st);
   if (e != hipSuccess) return e;
+  a.tiles = p.expand.tiles;
   if (a.rank % 8 == 0) return half ? launch_expand<DT, MT, true, true>(a, cus, st) : launch_expand<DT, MT, false, true>(a, cus, st);
   return half ? launch_expand<DT, MT, true, false>(a, cus, st) : launch_expand<DT, MT, false, false>(a, cus, st);
 }
@@ -496,7 +596,7 @@ extern "C" {
 int64_t fpsketch_adapters_workspace(int64_t t, int64_t k, int64_t n, int32_t count, int32_t rank) {
   int cus = 0;
   if (!adapter_dims(t, k, n, count, rank) || t == 0 || layer_device(&cus) != FPSK_OK) return 0;
-  return 4 * t * rank * cut_of(t, k, count, rank, cus).splits;
+  return space_of(plan_of(t, k, count, rank, false, cus), t);
 }
 
 fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, const void* B,
@@ -519,11 +619,11 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
   int cus = 0;
   const fpsketch_status s = layer_device(&cus);
   if (s != FPSK_OK) return s;
-  const Cut c = cut_of(t, k, count, rank, cus);
-  const int64_t need = 4 * t * rank * c.splits;
-  // work-groups of the two launches: 128 columns or 16 ranks at least, a compute unit's worth of
-  // ways and parts of k at most
-  if (static_cast<double>(c.tiles) * c.ways * std::max<double>((n + 127) / 128, c.rank_blocks * c.splits) * kThreads >= 4294967296.0) {
+  const Plan p = plan_of(t, k, count, rank, k % 8 == 0 && k <= kMaxLd && aligned(X, 16) && aligned(A, 16), cus);
+  const int64_t need = space_of(p, t);
+  // work-groups of the two launches
+  if (static_cast<double>(p.shrink.tiles) * p.shrink.ways * p.rank_blocks * p.splits * kThreads >= 4294967296.0 ||
+      (static_cast<double>(p.expand.tiles) * ((n + 127) / 128) + 64.0 * cus) * kThreads >= 4294967296.0) {
     return layer_error(FPSK_ESHAPE, "fpsketch_adapters: too many tiles");
   }
   if (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16)) {
@@ -546,6 +646,8 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
   a.count = count;
   a.rank = rank;
   a.V = static_cast<float*>(workspace);
+  a.ldv = p.ldv;
+  a.splits = p.splits;
   a.Y = Y;
   const auto st = static_cast<hipStream_t>(stream);
   hipError_t e;
@@ -554,9 +656,9 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
     e = dtype == FPSK_BF16 ? launch_k(tiny_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half})
                            : launch_k(tiny_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half});
   } else if (dtype == FPSK_BF16) {
-    e = c.mt == 2 ? launch_adapters<1, 2>(a, c, half, cus, st) : launch_adapters<1, 1>(a, c, half, cus, st);
+    e = p.expand.mt == 2 ? launch_adapters<1, 2>(a, p, half, cus, st) : launch_adapters<1, 1>(a, p, half, cus, st);
   } else {
-    e = c.mt == 2 ? launch_adapters<0, 2>(a, c, half, cus, st) : launch_adapters<0, 1>(a, c, half, cus, st);
+    e = p.expand.mt == 2 ? launch_adapters<0, 2>(a, p, half, cus, st) : launch_adapters<0, 1>(a, p, half, cus, st);
   }
   return launched(e, "fpsketch_adapters");
 }

@@ -127,8 +127,6 @@ struct Tile {
 // boundaries (rows a multiple of 8 long), 32-bit offsets within the tile (ld at most kMaxLd).  A
 // wave's 64 groups land in order, so the permutation is in the addresses.  Rows past the end repeat the last one, whose products
 // are not stored; for k past K the offset is one that the buffer's bounds turn into zeros.
-constexpr int64_t kMaxLd = int64_t{1} << 22;
-constexpr uint32_t kBound = 1u << 31, kOutside = ~15u;   // bytes of a buffer; an offset past them
 
 template <int R, int NT, int KD, bool KM, bool GATE>
 struct Stage {
@@ -522,90 +520,43 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_deep_kernel(MmArgs a) {
   w.store(a, p.m0, p.n0, p.split, 0);
 }
 
-// Up to 16 tokens: bound by reading W once, so that every wave streams W straight into fragments, 64 k
-// a step as 32 bytes a lane (a row's four lanes read a whole line), AHEAD steps under way.  A
-// work-group takes 16 columns of H and all tokens; each wave takes a run of k, so that it reads on in
-// its rows, and their sums meet in LDS.  One token, 4096 x 11008 BF16: 33.5 us = 5.4 TB/s (39.5 us with
-// the waves taking steps in turn and loads that bypass the caches, 36.1 us with three steps ahead);
-// the tiles take 44.8 us, and 46 us where this kernel with two row blocks took 43 us at 17 tokens and
-// 51 us at 32.
-template <int DT, int WAVES, int AHEAD>
-__global__ __launch_bounds__(64 * WAVES) void few_kernel(MmArgs a, int act) {
-  __shared__ __attribute__((aligned(16))) float red[WAVES][kFew][36];
+// Up to 16 tokens: bound by reading W once.  A work-group takes 16 columns of H and all tokens; each
+// wave streams a run of k of its gate rows, up rows and tokens, and the waves' sums meet in LDS.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void few_kernel(MmArgs a, int act) {
+  constexpr int kWaves = kThreads / 64, kBytes = WaveRows<1>::kBytes + WaveRows<2>::kBytes;
+  __shared__ __attribute__((aligned(16))) char r0[kWaves * kBytes];
+  __shared__ __attribute__((aligned(16))) char r1[kWaves * kBytes];
+  __shared__ __attribute__((aligned(16))) char r2[kWaves * kBytes];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   const int64_t j0 = static_cast<int64_t>(blockIdx.x) * 16;
-  // rows past the end repeat the last one; their sums are not stored
-  const int64_t m = lane & 15, j = j0 + (lane & 15), row = j < a.f ? j : a.f - 1;
-  const int64_t xo = (m < a.M ? m : a.M - 1) * a.K + 16 * g;
-  const int64_t wo[2] = {row * a.K + 16 * g, (row + a.f) * a.K + 16 * g};
-  u32x4 x[AHEAD + 1][2], w[AHEAD + 1][2][2];
-  auto fetch = [&](int b, int64_t s) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t k0 = 64 * s + 8 * h;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) w[b][u][h] = *reinterpret_cast<const u32x4_a2*>(a.B + wo[u] + k0);
-      x[b][h] = *reinterpret_cast<const u32x4_a2*>(a.A + xo + k0);
-    }
-    __builtin_amdgcn_sched_barrier(0);     // (else the loads sink to where they are used)
-  };
-  f32x4 acc[2] = {};
-  auto multiply = [&](int b) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) acc[u] = mfma32<DT>(w[b][u][h], x[b][h], acc[u]);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  const int64_t steps = a.K / 64, run = (steps + WAVES - 1) / WAVES;
-  int64_t s = wave * run < steps ? wave * run : steps, left = steps - s < run ? steps - s : run;
-  if (left > 0) {
-    // unconditional loads (behind a branch the compiler waits for those ahead too): past its run a
-    // wave reads the last step again
-    const int64_t last = s + left - 1;
-#pragma unroll
-    for (int b = 0; b < AHEAD; ++b) fetch(b, s + b < last ? s + b : last);
-    for (; left > AHEAD; left -= AHEAD + 1, s += AHEAD + 1) {
-#pragma unroll
-      for (int b = 0; b <= AHEAD; ++b) {
-        fetch((b + AHEAD) % (AHEAD + 1), s + b + AHEAD < last ? s + b + AHEAD : last);
-        multiply(b);
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < AHEAD; ++b) {
-      if (b < left) multiply(b);
-    }
-  }
-  if (wave == WAVES - 1 && 64 * steps < a.K) {            // the broken last step
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t k0 = 64 * steps + 8 * h, nv = a.K - k0 - 16 * g;
-      x[0][h] = load_ragged(a.A, xo + k0, nv, a.M * a.K);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) w[0][u][h] = load_ragged(a.B, wo[u] + k0, nv, a.N * a.K);
-    }
-    multiply(0);
-  }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) *reinterpret_cast<f32x4*>(&red[wave][lane & 15][16 * u + 4 * g]) = acc[u];
+  WaveRows<1> x;
+  WaveRows<2> w;
+  x.set(0, a.A, 0, a.M, a.lda);
+  w.set(0, a.B, j0, a.f, a.ldb);
+  w.set(1, a.B + a.f * a.ldb, j0, a.f, a.ldb);
+  f32x4 acc[1][2] = {};
+  const int64_t steps = (a.K + kStreamK - 1) / kStreamK, run = (steps + kWaves - 1) / kWaves * kStreamK;
+  const int64_t k0 = wave * run, k1 = k0 + run < a.K ? k0 + run : a.K;
+  wave_product<DT, 1, 2>(x, w, r0 + wave * kBytes, r1 + wave * kBytes, r2 + wave * kBytes, k0, k1, acc);
   __syncthreads();
-  for (int e = threadIdx.x; e < kFew * 16; e += 64 * WAVES) {
-    const int r = e / 16, c = e % 16;
-    if (r >= a.M || j0 + c >= a.f) continue;
-    float gate = 0.0f, up = 0.0f;
+  auto red = reinterpret_cast<float(*)[kFew][36]>(r0);
 #pragma unroll
-    for (int v = 0; v < WAVES; ++v) {
-      gate += red[v][r][c];
-      up += red[v][r][16 + c];
-    }
-    if (a.out != nullptr) {
-      a.out[r * a.N + j0 + c] = gate;
-      a.out[r * a.N + a.f + j0 + c] = up;
-    }
-    a.H[r * a.f + j0 + c] = to_half<DT>(gate_up<DT>(act, gate, up));
+  for (int u = 0; u < 2; ++u) *reinterpret_cast<f32x4*>(&red[wave][lane & 15][16 * u + 4 * g]) = acc[0][u];
+  __syncthreads();
+  const int r = threadIdx.x / 16, c = threadIdx.x % 16;
+  if (r >= a.M || j0 + c >= a.f) return;
+  float gate = 0.0f, up = 0.0f;
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    gate += red[v][r][c];
+    up += red[v][r][16 + c];
   }
+  if (a.out != nullptr) {
+    a.out[r * a.N + j0 + c] = gate;
+    a.out[r * a.N + a.f + j0 + c] = up;
+  }
+  a.H[r * a.f + j0 + c] = to_half<DT>(gate_up<DT>(act, gate, up));
 }
 
 // A product with an operand of fewer than 8 elements, which 16-byte loads do not fit: one output
@@ -943,7 +894,7 @@ hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
   }
   if constexpr (GATED) {
     if (c.few) {
-      FPSK_LAUNCH((few_kernel<DT, 4, 2>), dim3(static_cast<unsigned>(c.tiles_n)), dim3(256), 0, st, a, act);
+      FPSK_LAUNCH(few_kernel<DT>, dim3(static_cast<unsigned>(c.tiles_n)), dim3(kThreads), 0, st, a, act);
       return hipSuccess;
     }
   }
@@ -1005,13 +956,13 @@ GatedPlan plan_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t
   Space space{static_cast<char*>(workspace)};
   g.x = operand(X, t, d);
   g.w = operand(W, 2 * f, d);
-  const bool few = t <= kFew && t * d >= 8 && 2 * f * d >= 8;
   const int64_t odd = (g.x.fit ? 0 : t * d) + (g.w.fit ? 0 : 2 * f * d);
-  if (!few && worth_copies(odd, t, 2 * f, d)) {
+  if (worth_copies(odd, t, 2 * f, d)) {
     copy_padded(g.x, space, g.pad, g.pads);
     copy_padded(g.w, space, g.pad, g.pads);
   }
-  g.cut = cut_of(t, f, true, few, d, g.x.fit && g.w.fit, cus);
+  const bool fit = g.x.fit && g.w.fit;
+  g.cut = cut_of(t, f, true, fit && t <= kFew, d, fit, cus);
   g.part = static_cast<float*>(space.take(part_bytes(g.cut, t, 2 * f)));
   g.bytes = space.used;
   return g;

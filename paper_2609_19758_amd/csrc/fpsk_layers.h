@@ -17,6 +17,9 @@ fpsketch_status layer_error(fpsketch_status s, const char* detail) noexcept;
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef u16x4 u16x4_a2 __attribute__((aligned(2)));
+typedef u16x2 u16x2_a2 __attribute__((aligned(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef f32x2 f32x2_a4 __attribute__((aligned(4)));
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -70,6 +73,110 @@ __device__ __forceinline__ u32x4 load_ragged(const uint16_t* X, int64_t off, int
   if (s & 2) v = u32x4{v[1], v[2], v[3], 0u};
   if (s & 4) v = u32x4{v[2], v[3], 0u, 0u};
   return v & rag_keep(0, nv);
+}
+
+// Row-major operands streamed by one wave for itself: blocks of 16 rows, 64 k a stage, by loads that go
+// straight to LDS.  Eight lanes read a row's 128-byte line; as fragments (a lane 16 bytes of its own
+// row) the same bytes cost the address unit a cycle a lane, four times as many, which bounded these
+// kernels at 16 bytes a cycle and compute unit.  16-byte group c of row r is kept at c ^ ((r / 2) % 8),
+// so that a fragment's reads cover all banks.  Rows of whole groups on 16-byte boundaries, ld at most
+// kMaxLd; k past the end reads zeros (an offset that the buffer's bounds turn into zeros).
+constexpr int64_t kMaxLd = int64_t{1} << 22;
+constexpr uint32_t kBound = 1u << 31, kOutside = ~15u;   // bytes of a buffer; an offset past them
+constexpr int kStreamK = 64;
+
+template <int BLOCKS>
+struct WaveRows {
+  static constexpr int kBytes = BLOCKS * 16 * kStreamK * 2;   // a stage
+  static constexpr int kLoads = 2 * BLOCKS;
+  const char* base[BLOCKS];
+  uint32_t at[BLOCKS][2];
+  int kk;                  // k of the lane's group in rows 0 .. 7, with bit 5 the other way in 8 .. 15
+
+  // Block b: the 16 rows from `first` of a matrix of `rows`; rows past the end repeat the last one.
+  __device__ __forceinline__ void set(int b, const uint16_t* x, int64_t first, int64_t rows, int64_t ld) {
+    const int lane = threadIdx.x & 63;
+    const int64_t from = first < rows ? first : rows - 1;
+    base[b] = reinterpret_cast<const char*>(x + from * ld);
+    kk = 8 * ((lane & 7) ^ (lane >> 4));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = 8 * i + (lane >> 3), in = from + r < rows ? r : rows - 1 - from;
+      at[b][i] = static_cast<uint32_t>(2 * (in * ld + (kk ^ (32 * i))));
+    }
+  }
+
+  __device__ __forceinline__ void load(char* lds, int64_t k0, int64_t K) const {
+    const int left = static_cast<int>(K - k0 < kStreamK ? K - k0 : kStreamK);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      const char* from = base[b] + (left > 0 ? 2 * k0 : 0);
+      const __amdgpu_buffer_rsrc_t buffer =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, kBound, 0x00027000);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            buffer, (__attribute__((address_space(3))) void*)(lds + (2 * b + i) * 1024), 16,
+            (kk ^ (32 * i)) < left ? at[b][i] : kOutside, 0, 0, 0);
+      }
+    }
+  }
+
+  // Fragment of block b, k = 32 ks .. 32 ks + 31 of the stage.
+  static __device__ __forceinline__ u32x4 frag(const char* lds, int b, int ks) {
+    const int lane = threadIdx.x & 63, r = lane & 15;
+    return *reinterpret_cast<const u32x4*>(lds + b * 2048 + r * 128 + (((4 * ks + (lane >> 4)) ^ (r >> 1)) << 4));
+  }
+};
+
+// Waits until at most `left` of this wave's loads to LDS are under way.
+template <int left>
+__device__ __forceinline__ void stage_here() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(left) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// acc[i][j] += F_j X_i^T over k in [k0, k1), X_i and F_j blocks of 16 rows: a wave's own product, three
+// stages in its parts of r0, r1 and r2, two of them under way.
+template <int DT, int MT, int NT>
+__device__ __forceinline__ void wave_product(const WaveRows<MT>& x, const WaveRows<NT>& f, char* r0, char* r1,
+                                             char* r2, int64_t k0, int64_t k1, f32x4 (&acc)[MT][NT]) {
+  constexpr int kLoads = WaveRows<MT>::kLoads + WaveRows<NT>::kLoads;
+  auto load = [&](char* lds, int64_t k) {
+    x.load(lds, k, k1);
+    f.load(lds + WaveRows<MT>::kBytes, k, k1);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto step = [&](char* lds, int64_t next) {
+    stage_here<2 * kLoads>();
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 fx[MT], ff[NT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fx[i] = WaveRows<MT>::frag(lds, i, ks);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) ff[j] = WaveRows<NT>::frag(lds + WaveRows<MT>::kBytes, j, ks);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = mfma32<DT>(ff[j], fx[i], acc[i][j]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load(lds, next);                       // (the fragments are in registers)
+  };
+  if (k0 < k1) {
+    load(r0, k0);
+    load(r1, k0 + kStreamK);
+    load(r2, k0 + 2 * kStreamK);
+    for (int64_t k = k0; k < k1; k += 3 * kStreamK) {   // (past k1 the stages hold zeros)
+      step(r0, k + 3 * kStreamK);
+      step(r1, k + 4 * kStreamK);
+      step(r2, k + 5 * kStreamK);
+    }
+  }
+  stage_here<0>();                         // no load outlives the product
 }
 
 // 1 / (1 + e^-x).  The hardware's exponential and reciprocal are within a few units of FP32's last
