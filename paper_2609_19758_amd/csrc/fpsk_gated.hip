@@ -108,13 +108,14 @@ struct Tile {
   static __device__ __forceinline__ u32x4 frag(const char* lds, int n0, int ks) {
     const int lane = threadIdx.x & 63;
     if constexpr (KM) {
+      // (each address in one step from the array: behind a second one the compiler no longer sees
+      // which buffer is read, and waits for the loads into the other)
       const int h = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
-      const int k = 32 * ks + 8 * (lane >> 4) + ((lane & 15) >> 2);
-      const char* p = lds + k * (2 * R) + (((n0 >> 4) ^ h) << 5) + 8 * (lane & 3);
+      const int at = (32 * ks + 8 * (lane >> 4) + ((lane & 15) >> 2)) * (2 * R) + (((n0 >> 4) ^ h) << 5) + 8 * (lane & 3);
       typedef __attribute__((address_space(3))) s16x4* lp;
-      const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p)));
+      const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(lds + at)));
       const u32x2 b = __builtin_bit_cast(
-          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * (2 * R))));
+          u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(lds + (at + 8 * R))));
       return u32x4{a[0], a[1], b[0], b[1]};
     } else {
       const int r = n0 + (lane & 15), c = 4 * ks + (lane >> 4);
