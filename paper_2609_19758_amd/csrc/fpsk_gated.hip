@@ -15,7 +15,6 @@
 #include "fpsk_layers.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace fpsk {
 
@@ -124,17 +123,16 @@ struct Tile {
   }
 };
 
-// A stage: the same tile KD deep, filled by loads that go straight to LDS: 16-byte groups on 16-byte
+// A stage: the same tile filled by loads that go straight to LDS: 16-byte groups on 16-byte
 // boundaries (rows a multiple of 8 long), 32-bit offsets within the tile (ld at most kMaxLd).  A
 // wave's 64 groups land in order, so the permutation is in the addresses.  Rows past the end repeat the last one, whose products
 // are not stored; for k past K the offset is one that the buffer's bounds turn into zeros.
 
-template <int R, int NT, int KD, bool KM, bool GATE>
+template <int R, int NT, bool KM, bool GATE>
 struct Stage {
-  static_assert(KM || KD == kBK, "half a line of a row would come from L2 twice");
   typedef Tile<R, NT, KM, GATE> T;
-  static constexpr int kBytes = R * KD * 2;
-  static constexpr int kLoads = R * KD / 8 / NT;
+  static constexpr int kBytes = R * kBK * 2;
+  static constexpr int kLoads = R * kBK / 8 / NT;
   static constexpr int kRows = 8 * NT / R;   // K-major: k rows per load
   static_assert(kLoads >= 1 && NT % 128 == 0 && (KM ? kRows : NT / 8) % 16 == 0,
                 "the permutation is the same for every load");
@@ -172,7 +170,7 @@ struct Stage {
   // The stage at k0, zeros from K on (all of it where k0 >= K).
   __device__ __forceinline__ void load(char* lds, int64_t k0, int64_t K) const {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int left = static_cast<int>(K - k0 < KD ? K - k0 : KD);
+    const int left = static_cast<int>(K - k0 < kBK ? K - k0 : kBK);
     // (past K the base itself must not run on: nothing is read there, but it stays an address)
     const char* from = base + (left > 0 ? k0 : 0) * step;
     const __amdgpu_buffer_rsrc_t buffer =
@@ -221,14 +219,14 @@ __device__ __forceinline__ void store4h(uint16_t* row, int64_t j, int64_t n, u16
   }
 }
 
-// Work-groups are dealt to the 8 XCDs in turn; each XCD gets neighbouring tiles, in bands of 8 rows
+// Work-groups are dealt to the 8 XCDs in turn; each XCD gets neighbouring tiles, in bands of 4 rows
 // of tiles, so that its L2 holds the operands' tiles that they share.
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
   const uint32_t per = tm * tn / 8;
   if (b < 8 * per) b = (b % 8) * per + b / 8;
-  const uint32_t band = b / (8 * tn), first = 8 * band;
-  const uint32_t height = tm - first < 8 ? tm - first : 8;
-  const uint32_t in = b - band * 8 * tn;
+  const uint32_t band = b / (4 * tn), first = 4 * band;
+  const uint32_t height = tm - first < 4 ? tm - first : 4;
+  const uint32_t in = b - band * 4 * tn;
   *n = in / height;
   *m = first + in - *n * height;
 }
@@ -407,8 +405,8 @@ __device__ __forceinline__ void stages_ready() {
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) {
   typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
-  typedef Stage<BM, W::NT, kBK, AKM, false> SA;
-  typedef Stage<BN, W::NT, kBK, BKM, GATED> SB;
+  typedef Stage<BM, W::NT, AKM, false> SA;
+  typedef Stage<BN, W::NT, BKM, GATED> SB;
   __shared__ __attribute__((aligned(16))) char a0[SA::kBytes];
   __shared__ __attribute__((aligned(16))) char b0[SB::kBytes];
   __shared__ __attribute__((aligned(16))) char a1[SA::kBytes];
@@ -438,87 +436,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) 
   stages_ready<0>();                       // no load outlives the kernel
   if (k < p.k1) w.multiply_ahead(a0, b0);
   w.store(a, p.m0, p.n0, p.split, act);
-}
-
-// Both operands K-major (dW): five stages of 32 k, stage s in buffer s % 5.  While one is multiplied
-// the next is there already, so that its first fragments are read before the barrier, and three are
-// under way; the stages past K that fill the last turn hold zeros.  22016 x 4096 x 2048: 383 us with
-// two buffers of 64 k, 364 us.  (A row-major operand would read half a line per stage: 747 -> 781 us
-// at 4096 x 4096 x 22016, and 912 us with the halves of a line loaded together.)
-template <int DT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void mm_deep_kernel(MmArgs a) {
-  typedef Wave<DT, BM, BN, WM, WN, true, true, false> W;
-  constexpr int KD = 32;
-  typedef Stage<BM, W::NT, KD, true, false> SA;
-  typedef Stage<BN, W::NT, KD, true, false> SB;
-  constexpr int MT = W::MT, NTL = W::NTL, kStageLoads = SA::kLoads + SB::kLoads;
-  static_assert(MT >= NTL, "");
-  __shared__ __attribute__((aligned(16))) char a0[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char a1[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char a2[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char a3[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char a4[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char b0[SB::kBytes];
-  __shared__ __attribute__((aligned(16))) char b1[SB::kBytes];
-  __shared__ __attribute__((aligned(16))) char b2[SB::kBytes];
-  __shared__ __attribute__((aligned(16))) char b3[SB::kBytes];
-  __shared__ __attribute__((aligned(16))) char b4[SB::kBytes];
-  const Part p = part_of<BM, BN, false>(a);
-  SA sa;
-  SB sb;
-  sa.init(a.A, p.m0, a.lda, a.lda, 0);
-  sb.init(a.B, p.n0, a.ldb, a.ldb, 0);
-  W w;
-  w.init();
-  auto load = [&](char* la, char* lb, int64_t k) {
-    sa.load(la, k, p.k1);
-    sb.load(lb, k, p.k1);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  u32x4 fa[2], fb[NTL];                    // the first two row blocks and all of B
-  // Multiplies the stage at la, lb and reads the first fragments of the next from na, nb; the loads
-  // at k go to where the stage before was, oa, ob.
-  auto step = [&](const char* la, const char* na, const char* nb, char* oa, char* ob, int64_t k) {
-    stages_ready<2 * kStageLoads>();
-    load(oa, ob, k);
-    u32x4 f[3], ga[2], gb[NTL];
-    f[0] = fa[0];
-    f[1] = fa[1];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if (i + 2 < MT) {
-        f[(i + 2) % 3] = W::TA::frag(la, w.wm + 16 * (i + 2), 0);
-      } else {
-        ga[i + 2 - MT] = W::TA::frag(na, w.wm + 16 * (i + 2 - MT), 0);
-      }
-      if (i >= MT - NTL) gb[i - (MT - NTL)] = W::TB::frag(nb, w.wn + 16 * (i - (MT - NTL)), 0);
-#pragma unroll
-      for (int j = 0; j < NTL; ++j) w.acc[i][j] = mfma32<DT>(fb[j], f[i % 3], w.acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    fa[0] = ga[0];
-    fa[1] = ga[1];
-#pragma unroll
-    for (int j = 0; j < NTL; ++j) fb[j] = gb[j];
-  };
-  load(a0, b0, p.k0);
-  load(a1, b1, p.k0 + KD);
-  load(a2, b2, p.k0 + 2 * KD);
-  load(a3, b3, p.k0 + 3 * KD);
-  stages_ready<3 * kStageLoads>();
-  fa[0] = W::TA::frag(a0, w.wm, 0);
-  fa[1] = W::TA::frag(a0, w.wm + 16, 0);
-#pragma unroll
-  for (int j = 0; j < NTL; ++j) fb[j] = W::TB::frag(b0, w.wn + 16 * j, 0);
-  for (int64_t k = p.k0; k < p.k1; k += 5 * KD) {
-    step(a0, a1, b1, a4, b4, k + 4 * KD);
-    step(a1, a2, b2, a0, b0, k + 5 * KD);
-    step(a2, a3, b3, a1, b1, k + 6 * KD);
-    step(a3, a4, b4, a2, b2, k + 7 * KD);
-    step(a4, a0, b0, a3, b3, k + 8 * KD);
-  }
-  stages_ready<0>();                       // no load outlives the kernel
-  w.store(a, p.m0, p.n0, p.split, 0);
 }
 
 // Up to 16 tokens: bound by reading W once.  A work-group takes 16 columns of H and all tokens; each
@@ -901,11 +818,7 @@ hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
   }
   const dim3 grid(static_cast<unsigned>(c.tiles_m * c.tiles_n * c.splits));
   if (c.big) {
-    if constexpr (AKM && BKM) {
-      FPSK_LAUNCH((mm_deep_kernel<DT, 256, 256, 2, 4>), grid, dim3(512), 0, st, a);
-    } else {
-      FPSK_LAUNCH((mm_kernel<DT, 256, 256, 2, 4, AKM, BKM, GATED>), grid, dim3(512), 0, st, a, act);
-    }
+    FPSK_LAUNCH((mm_kernel<DT, 256, 256, 2, 4, AKM, BKM, GATED>), grid, dim3(512), 0, st, a, act);
   } else if (c.direct) {
     FPSK_LAUNCH((mm_kernel<DT, 128, 128, 2, 2, AKM, BKM, GATED>), grid, dim3(256), 0, st, a, act);
   } else {
