@@ -332,12 +332,12 @@ struct Part {
 };
 
 template <int BM, int BN, bool GATED>
-__device__ __forceinline__ Part part_of(const MmArgs& a) {
+__device__ __forceinline__ Part part_of(const MmArgs& a, uint32_t block) {
   // (32 bits: a launch has fewer work-groups, and a 64-bit division takes a microsecond)
   const auto rows = static_cast<uint32_t>(a.tiles_m), cols = static_cast<uint32_t>(a.tiles_n);
-  const uint32_t split = blockIdx.x / (rows * cols);
+  const uint32_t split = block / (rows * cols);
   uint32_t tm, tn;
-  tile_of(blockIdx.x - split * rows * cols, rows, cols, &tm, &tn);
+  tile_of(block - split * rows * cols, rows, cols, &tm, &tn);
   Part p;
   p.split = split;
   p.m0 = static_cast<int64_t>(tm) * BM;
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_ragged_kernel(MmArgs a, in
   typedef typename W::TB TB;
   __shared__ __attribute__((aligned(16))) char lds_a[2][TA::kBytes];
   __shared__ __attribute__((aligned(16))) char lds_b[2][TB::kBytes];
-  const Part p = part_of<BM, BN, GATED>(a);
+  const Part p = part_of<BM, BN, GATED>(a, blockIdx.x);
   TA ta;
   TB tb;
   ta.init(a.A, p.m0, a.M, AKM ? a.M : a.K, 0, a.M * a.K);
@@ -403,15 +403,12 @@ __device__ __forceinline__ void stages_ready() {
 // products.  A buffer is an array of its own, so that the compiler knows loads into one apart from
 // reads of the other.
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
-__global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) {
+__device__ __forceinline__ void mm_tile(const MmArgs& a, int act, uint32_t block, char* a0, char* b0,
+                                        char* a1, char* b1) {
   typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
   typedef Stage<BM, W::NT, AKM, false> SA;
   typedef Stage<BN, W::NT, BKM, GATED> SB;
-  __shared__ __attribute__((aligned(16))) char a0[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char b0[SB::kBytes];
-  __shared__ __attribute__((aligned(16))) char a1[SA::kBytes];
-  __shared__ __attribute__((aligned(16))) char b1[SB::kBytes];
-  const Part p = part_of<BM, BN, GATED>(a);
+  const Part p = part_of<BM, BN, GATED>(a, block);
   SA sa;
   SB sb;
   sa.init(a.A, p.m0, AKM ? a.lda : a.M, a.lda, 0);
@@ -436,6 +433,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) 
   stages_ready<0>();                       // no load outlives the kernel
   if (k < p.k1) w.multiply_ahead(a0, b0);
   w.store(a, p.m0, p.n0, p.split, act);
+}
+
+template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mm_kernel(MmArgs a, int act) {
+  __shared__ __attribute__((aligned(16))) char a0[BM * kBK * 2];
+  __shared__ __attribute__((aligned(16))) char b0[BN * kBK * 2];
+  __shared__ __attribute__((aligned(16))) char a1[BM * kBK * 2];
+  __shared__ __attribute__((aligned(16))) char b1[BN * kBK * 2];
+  mm_tile<DT, BM, BN, WM, WN, AKM, BKM, GATED>(a, act, blockIdx.x, a0, b0, a1, b1);
+}
+
+// dX and dW in one launch: tiles of 128 x 128 are taken where they do not fill the chip for long, and
+// two launches would leave it part empty twice (1000 x 512 x 1024: 32 us in two, 20 us; 333 x 1000 x
+// 2731 with its padded copies: 36 and 28 us).
+template <int DT>
+__global__ __launch_bounds__(256, 2) void mm_pair_kernel(MmArgs dx, MmArgs dw, uint32_t first) {
+  __shared__ __attribute__((aligned(16))) char a0[128 * kBK * 2];
+  __shared__ __attribute__((aligned(16))) char b0[128 * kBK * 2];
+  __shared__ __attribute__((aligned(16))) char a1[128 * kBK * 2];
+  __shared__ __attribute__((aligned(16))) char b1[128 * kBK * 2];
+  if (blockIdx.x < first) {
+    mm_tile<DT, 128, 128, 2, 2, false, true, false>(dx, 0, blockIdx.x, a0, b0, a1, b1);
+  } else {
+    mm_tile<DT, 128, 128, 2, 2, true, true, false>(dw, 0, blockIdx.x - first, a0, b0, a1, b1);
+  }
 }
 
 // Up to 16 tokens: bound by reading W once.  A work-group takes 16 columns of H and all tokens; each
@@ -740,6 +762,16 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct
   return c;
 }
 
+// K in fewer parts, but two, where another product of the same launch leaves `room` work-groups only
+// (500 x 2048 x 2048: 42 us with each product cut for itself, 33 us).
+void fewer_parts(Cut& c, int64_t K, int64_t room) {
+  const int64_t most = std::max<int64_t>(2, room / (c.tiles_m * c.tiles_n));
+  if (c.splits <= most) return;
+  const int64_t steps = (K + kBK - 1) / kBK, per = (steps + most - 1) / most;
+  c.kslice = per * kBK;
+  c.splits = static_cast<int>((steps + per - 1) / per);
+}
+
 // An operand that the loads to LDS fit as it is: rows of whole 16-byte groups on 16-byte boundaries.
 bool fits(const void* p, int64_t ld) { return ld % 8 == 0 && aligned(p, 16); }
 
@@ -797,12 +829,32 @@ hipError_t launch_pad(const PadArgs& pad, int pads, hipStream_t st) {
   return hipSuccess;
 }
 
-template <int DT, bool AKM, bool BKM, bool GATED>
-hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
+MmArgs cut(MmArgs a, const Cut& c) {
   a.tiles_m = c.tiles_m;
   a.tiles_n = c.tiles_n;
   a.splits = c.splits;
   a.kslice = c.kslice;
+  return a;
+}
+
+template <int DT, bool GATED>
+hipError_t launch_sum(const MmArgs& a, const Cut& c, int act, hipStream_t st) {
+  if (c.splits > 1) {
+    const int64_t count = a.M * (GATED ? a.f : a.N);
+    const bool four = (GATED ? a.f : a.M * a.N) % 4 == 0;
+    const auto g = static_cast<unsigned>(std::min<int64_t>((count / (four ? 4 : 1) + kThreads - 1) / kThreads, 8192));
+    if (four) {
+      FPSK_LAUNCH((mm_sum_kernel<DT, GATED, 4>), dim3(g), dim3(kThreads), 0, st, a, act);
+    } else {
+      FPSK_LAUNCH((mm_sum_kernel<DT, GATED, 1>), dim3(g), dim3(kThreads), 0, st, a, act);
+    }
+  }
+  return hipSuccess;
+}
+
+template <int DT, bool AKM, bool BKM, bool GATED>
+hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
+  a = cut(a, c);
   if (!c.direct && !c.few && a.K > 0 && (a.M * a.K < 8 || a.N * a.K < 8)) {
     const int64_t count = a.M * (GATED ? a.f : a.N);
     const auto g = static_cast<unsigned>(std::min<int64_t>((count + kThreads - 1) / kThreads, 8192));
@@ -824,17 +876,18 @@ hipError_t launch_mm(MmArgs a, const Cut& c, int act, hipStream_t st) {
   } else {
     FPSK_LAUNCH((mm_ragged_kernel<DT, 128, 128, 2, 2, AKM, BKM, GATED>), grid, dim3(256), 0, st, a, act);
   }
-  if (c.splits > 1) {
-    const int64_t count = a.M * (GATED ? a.f : a.N);
-    const bool four = (GATED ? a.f : a.M * a.N) % 4 == 0;
-    const auto g = static_cast<unsigned>(std::min<int64_t>((count / (four ? 4 : 1) + kThreads - 1) / kThreads, 8192));
-    if (four) {
-      FPSK_LAUNCH((mm_sum_kernel<DT, GATED, 4>), dim3(g), dim3(kThreads), 0, st, a, act);
-    } else {
-      FPSK_LAUNCH((mm_sum_kernel<DT, GATED, 1>), dim3(g), dim3(kThreads), 0, st, a, act);
-    }
-  }
-  return hipSuccess;
+  return launch_sum<DT, GATED>(a, c, act, st);
+}
+
+template <int DT>
+hipError_t launch_pair(MmArgs x, const Cut& cx, MmArgs w, const Cut& cw, hipStream_t st) {
+  x = cut(x, cx);
+  w = cut(w, cw);
+  const auto first = static_cast<unsigned>(cx.tiles_m * cx.tiles_n * cx.splits);
+  const auto second = static_cast<unsigned>(cw.tiles_m * cw.tiles_n * cw.splits);
+  FPSK_LAUNCH(mm_pair_kernel<DT>, dim3(first + second), dim3(256), 0, st, x, w, first);
+  const hipError_t e = launch_sum<DT, false>(x, cx, 0, st);
+  return e != hipSuccess ? e : launch_sum<DT, false>(w, cw, 0, st);
 }
 
 bool dims_ok(int64_t t, int64_t d, int64_t f) {
@@ -882,14 +935,15 @@ GatedPlan plan_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t
   return g;
 }
 
-// The same for fpsketch_gated_products; the two products run one after the other and share the room
-// for their parts.
+// The same for fpsketch_gated_products.  Two products that run one after the other share the room for
+// their parts.
 struct ProductsPlan {
   Operand p, x, w, xw;     // dP, X, W; dP as dX takes it
   PadArgs pad{};
   int pads = 0;
   Cut dx, dw;
-  float* part;
+  bool pair;
+  float *part_x, *part_w;
   int64_t bytes;
 };
 
@@ -900,27 +954,32 @@ ProductsPlan plan_products(const void* dP, const void* X, const void* W, int64_t
   g.p = operand(dP, t, 2 * f);
   g.x = operand(X, t, d);
   g.w = operand(W, 2 * f, d);
+  // How each is computed does not depend on whether the other is asked for, so that it has the same
+  // bits either way.
   const int64_t odd_p = g.p.fit ? 0 : 2 * t * f;
-  // dP is copied once for both
-  const bool dx = need_dx && worth_copies(odd_p + (g.w.fit ? 0 : 2 * f * d), t, d, 2 * f);
-  const bool dw = need_dw && worth_copies((dx ? 0 : odd_p) + (g.x.fit ? 0 : t * d), 2 * f, d, t);
-  g.xw = g.p;
-  if (dx || dw) copy_padded(g.p, space, g.pad, g.pads);
-  if (dx) {
-    g.xw = g.p;
-    copy_padded(g.w, space, g.pad, g.pads);
+  const bool direct_x = worth_copies(odd_p + (g.w.fit ? 0 : 2 * f * d), t, d, 2 * f);
+  const bool direct_w = worth_copies(odd_p + (g.x.fit ? 0 : t * d), 2 * f, d, t);
+  g.dx = cut_of(std::max<int64_t>(t, 1), d, false, false, 2 * f, direct_x, cus);
+  g.dw = cut_of(2 * f, d, false, false, t, direct_w, cus);
+  const bool take_x = need_dx && t > 0 && direct_x, take_w = need_dw && direct_w;
+  const Operand p = g.p;
+  if (take_x || take_w) copy_padded(g.p, space, g.pad, g.pads);   // once for both
+  g.xw = take_x ? g.p : p;
+  if (!take_w) g.p = p;
+  if (take_x) copy_padded(g.w, space, g.pad, g.pads);
+  if (take_w) copy_padded(g.x, space, g.pad, g.pads);
+  if (!g.dx.big && !g.dw.big) {
+    fewer_parts(g.dx, 2 * f, 2 * cus - g.dw.tiles_m * g.dw.tiles_n);
+    fewer_parts(g.dw, t, 2 * cus - g.dx.tiles_m * g.dx.tiles_n);
   }
-  if (dw) {
-    copy_padded(g.x, space, g.pad, g.pads);
+  g.pair = take_x && take_w && !g.dx.big && !g.dw.big;
+  const int64_t px = need_dx && t > 0 ? part_bytes(g.dx, t, d) : 0, pw = need_dw ? part_bytes(g.dw, 2 * f, d) : 0;
+  if (g.pair) {
+    g.part_x = static_cast<float*>(space.take(px));
+    g.part_w = static_cast<float*>(space.take(pw));
   } else {
-    g.p = operand(dP, t, 2 * f);
+    g.part_x = g.part_w = static_cast<float*>(space.take(std::max(px, pw)));
   }
-  g.dx = cut_of(std::max<int64_t>(t, 1), d, false, false, 2 * f, g.xw.fit && g.w.fit, cus);
-  g.dw = cut_of(2 * f, d, false, false, t, g.p.fit && g.x.fit, cus);
-  int64_t part = 0;
-  if (need_dx && t > 0) part = part_bytes(g.dx, t, d);
-  if (need_dw) part = std::max(part, part_bytes(g.dw, 2 * f, d));
-  g.part = static_cast<float*>(space.take(part));
   g.bytes = space.used;
   return g;
 }
@@ -1078,31 +1137,35 @@ fpsketch_status fpsketch_gated_products(const void* dP, const void* X, const voi
   if (!disjoint(in, out)) return layer_error(FPSK_EINVAL, "fpsketch_gated_products: an output overlaps another argument");
   const auto st = static_cast<hipStream_t>(stream);
   hipError_t e = launch_pad(g.pad, g.pads, st);
-  MmArgs a{};
-  a.part = g.part;
+  MmArgs x{}, w{};
+  x.A = g.xw.p;
+  x.B = g.w.p;
+  x.M = t;
+  x.N = d;
+  x.K = 2 * f;
+  x.lda = g.xw.ld;
+  x.ldb = g.w.ld;
+  x.out = dX;
+  x.part = g.part_x;
+  w.A = g.p.p;
+  w.B = g.x.p;
+  w.M = 2 * f;
+  w.N = d;
+  w.K = t;
+  w.lda = g.p.ld;
+  w.ldb = g.x.ld;
+  w.out = dW;
+  w.part = g.part_w;
+  const bool bf16 = dtype == FPSK_BF16;
+  if (e == hipSuccess && g.pair) {
+    e = bf16 ? launch_pair<1>(x, g.dx, w, g.dw, st) : launch_pair<0>(x, g.dx, w, g.dw, st);
+    return launched(e, "fpsketch_gated_products");
+  }
   if (e == hipSuccess && need_dx && t > 0) {
-    a.A = g.xw.p;
-    a.B = g.w.p;
-    a.M = t;
-    a.N = d;
-    a.K = 2 * f;
-    a.lda = g.xw.ld;
-    a.ldb = g.w.ld;
-    a.out = dX;
-    e = dtype == FPSK_BF16 ? launch_mm<1, false, true, false>(a, g.dx, 0, st)
-                           : launch_mm<0, false, true, false>(a, g.dx, 0, st);
+    e = bf16 ? launch_mm<1, false, true, false>(x, g.dx, 0, st) : launch_mm<0, false, true, false>(x, g.dx, 0, st);
   }
   if (e == hipSuccess && need_dw) {
-    a.A = g.p.p;
-    a.B = g.x.p;
-    a.M = 2 * f;
-    a.N = d;
-    a.K = t;
-    a.lda = g.p.ld;
-    a.ldb = g.x.ld;
-    a.out = dW;
-    e = dtype == FPSK_BF16 ? launch_mm<1, true, true, false>(a, g.dw, 0, st)
-                           : launch_mm<0, true, true, false>(a, g.dw, 0, st);
+    e = bf16 ? launch_mm<1, true, true, false>(w, g.dw, 0, st) : launch_mm<0, true, true, false>(w, g.dw, 0, st);
   }
   return launched(e, "fpsketch_gated_products");
 }

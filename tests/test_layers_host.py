@@ -321,7 +321,7 @@ def launches(h):
             h.rt.rt_reset()
             assert C(h, t=t, d=d, f=f)() == fk.OK
             seen |= {re.sub(r".*12_GLOBAL__N_1\d+(\w+?_kernel).*", r"\1", k) for k, _ in h.kernels()}
-    assert {"few_kernel", "mm_kernel", "mm_sum_kernel", "pad_kernel"} <= seen, seen
+    assert {"few_kernel", "mm_kernel", "mm_pair_kernel", "mm_sum_kernel", "pad_kernel"} <= seen, seen
     # the longest batches: refused or launched, never a grid the runtime does not take
     for t, d, f in itertools.product([1 << 20, (1 << 31) - 1], [1, 64, 512], [1, 64, 256]):
         for C in (Gated, Narrow, Grad, Products, Adapters):
