@@ -77,10 +77,13 @@ class _Call:
         if stream is None and device.index == torch._C._cuda_getDevice():
             self.stream = torch._C._cuda_getCurrentRawStream(device.index)
             return
+        if getattr(stream, "device", device) != device:
+            raise ValueError(f"stream: on {stream.device}, the operands are on {device}")
+        given = None if stream is None else fk._stream(stream)
         self.stack = contextlib.ExitStack()
         self.stack.enter_context(torch.cuda.device(device))
         now = torch.cuda.current_stream().cuda_stream
-        self.stream = now if stream is None else fk._stream(stream)
+        self.stream = now if given is None else given
         if self.stream != now:
             self.stack.enter_context(torch.cuda.stream(
                 torch.cuda.ExternalStream(self.stream, device=device)))

@@ -55,6 +55,65 @@ def test_large_products_are_exact(fl, t, d, f, fmt):
     assert torch.equal(dW, (dP.double().t() @ X.double()).float())
 
 
+@pytest.mark.parametrize("fmt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("t,d,f", [(333, 1000, 2731), (2000, 256, 512), (500, 2048, 2048), (40, 4000, 1000),
+                                   (1500, 1023, 2049), (1, 64, 4096), (7, 4104, 8), (2600, 16, 64)])
+def test_one_backward_product_has_the_bits_it_has_beside_the_other(fl, t, d, f, fmt):
+    """Both in one launch, and both in parts, where they are small; exact, as their sums stay below 2^24."""
+    g = gen(3 * t + d + f)
+    X, W, dP = ints(g, t, d, to=fmt), ints(g, 2 * f, d, to=fmt), ints(g, t, 2 * f, to=fmt)
+    dX, dW = fl.gated_products(dP, X, W)
+    assert torch.equal(dX, (dP.double() @ W.double()).float())
+    assert torch.equal(dW, (dP.double().t() @ X.double()).float())
+    X, W, dP = gauss(g, t, d, to=fmt), gauss(g, 2 * f, d, to=fmt), gauss(g, t, 2 * f, to=fmt)
+    dX, dW = fl.gated_products(dP, X, W)
+    assert torch.equal(fl.gated_products(dP, X, W, need_dw=False)[0], dX)
+    assert torch.equal(fl.gated_products(dP, X, W, need_dx=False)[1], dW)
+    outs = torch.zeros_like(dX), torch.zeros_like(dW)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fl.gated_products(dP, X, W, dX=outs[0], dW=outs[1])
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        again = fl.gated_products(dP, X, W)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], dX) and torch.equal(outs[1], dW)
+        assert torch.equal(again[0], dX) and torch.equal(again[1], dW)
+
+
+@pytest.mark.parametrize("fmt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rank", [248, 255, 256])
+def test_long_batches_of_the_widest_adapters(fl, rank, fmt):
+    """Tiles of 32 rows at the largest rank, whose sums need more than 64 KiB of LDS; eager and captured."""
+    g = gen(rank)
+    t, k, n, count = 1060, 192, 200, 3
+    X, C = gauss(g, t, k, to=fmt), gauss(g, t, n)
+    A, B = gauss(g, count, rank, k, std=1 / math.sqrt(k), to=fmt), gauss(g, count, n, rank, std=0.3, to=fmt)
+    index = (torch.arange(t, device="cuda") // 100 % (count + 1) - 1).int()
+    scale = torch.tensor([1.5, -0.5, 2.0], device="cuda")
+    Y = fl.adapters(C, X, A, B, index, scale, out="f32")
+    want, D = C.double(), C.double().abs()
+    for a in range(count):
+        r = (index == a).nonzero().flatten()
+        x, p, q, s = X[r].double(), A[a].double().t().contiguous(), B[a].double().t().contiguous(), float(scale[a])
+        want[r] += s * ((x @ p) @ q)
+        D[r] += abs(s) * ((x.abs() @ p.abs()) @ q.abs())
+    # k products and rank terms, each 2u; the rank's sums enter in two half words (2^-21, bf16 2^-16)
+    tol = D * ((k + rank + 8) * 2 * U + (2.0 ** -16 if fmt is torch.bfloat16 else 2.0 ** -21))
+    assert bool(((Y.double() - want).abs() <= tol).all())
+    out = torch.zeros_like(Y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fl.adapters(C, X, A, B, index, scale, out="f32", Y=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, Y)
+
+
 # ---- with the verifier ---------------------------------------------------------------------
 
 

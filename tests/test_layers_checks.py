@@ -103,3 +103,10 @@ def test_heads_grad_refuses():
     refuses("dq: \\(3, 16\\)", fl.heads_grad, z(3, 16), dk, dv, None, pos, freq)
     refuses("2 query and 0 key heads", fl.heads_grad, dq, z(3, 0, 8), z(3, 0, 8), None, pos, freq)
     refuses("expected a GPU tensor", fl.heads_grad, dq, dk, dv, None, pos, freq)
+
+
+def test_a_stream_of_another_gpu_is_refused():
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 7
+
+    refuses("stream: on cuda:1, the operands are on cuda:0", fl._Call, torch.device("cuda", 0), Stream())
