@@ -29,8 +29,7 @@ struct AdapterArgs {
   int64_t tiles;
   int ways;                // work-groups that share a tile's adapters
   int splits;              // parts of k
-  int blocks;              // rank blocks (shrink) or column blocks (expand)
-  int64_t cols;            // columns per column block
+  int blocks;              // rank blocks (shrink), or work-groups that share a tile's columns (expand)
 };
 
 // Both kernels take tiles of neighbouring rows as they come, in turn over the adapters that a tile's rows name: an adapter's factor multiplies the whole tile on the matrix
@@ -237,14 +236,16 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_ragged_kernel(Adapte
   });
 }
 
-// Y = C + s V B^T on a tile of 16 MT rows and `cols` columns, 128 NC of them at a time.  Bound by C
+constexpr int kColumns = 128;   // of a work-group at a time, 32 per wave
+
+// Y = C + s V B^T on a tile of 16 MT rows.  Bound by C
 // and Y, whose loads and stores are whole lines: the columns of a 32-wide block are dealt to two
 // products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as two half
 // words, hi + lo, so that 16 (BF16) or 22 (FP16) of its bits count against the exact factor B; in
 // FP16 a row is first scaled by a power of two to where both words are in range.
 //
 // WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
-template <int DT, int MT, int NC, bool HALF, bool WHOLE>
+template <int DT, int MT, bool HALF, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, PER = kThreads / TR;      // threads per row of V
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -255,11 +256,10 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
   float* back = sums + TR * rp;                         // TR: what undoes the scaling
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   unsigned b = blockIdx.x;
-  const int64_t c0 = static_cast<int64_t>(b % a.blocks) * a.cols;
+  const int64_t c0 = static_cast<int64_t>(b % a.blocks) * kColumns;
   b /= a.blocks;
   const int64_t row0 = static_cast<int64_t>(b % a.tiles) * TR;
   const int way = static_cast<int>(b / a.tiles);
-  const int64_t c1 = c0 + a.cols < a.n ? c0 + a.cols : a.n;
 
   for_adapters<TR>(a, row0, way, [&](int which, uint64_t mask) {
     const bool mine = which >= 0 && which < a.count;
@@ -322,53 +322,44 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
       for (int i = 0; i < MT; ++i) scale[i] = a.scale[which] * back[16 * i + (lane & 15)];
     }
 
-    // FULL: the wave's columns all lie in the row.
+    // FULL: the wave's 32 columns all lie in the row.
     auto columns = [&](int64_t n0, auto full) {
       constexpr bool FULL = decltype(full)::value;
-      u32x4 f[NC][2];
+      u32x4 f[2];
       auto fetch = [&](int s) {
 #pragma unroll
-        for (int q = 0; q < NC; ++q) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            // row i of the product's 16 is column 8 (i / 4) + 4 h + i % 4 of the block
-            const int64_t col = n0 + 32 * q + 8 * ((lane & 15) >> 2) + 4 * h + (lane & 3);
-            const bool ok = (FULL || col < a.n) && s + 8 * g < a.rank;
-            const int64_t at = (base + col) * a.rank + s + 8 * g;
-            if constexpr (WHOLE) {
-              f[q][h] = *reinterpret_cast<const u32x4_a2*>(a.B + (ok ? at : 0));
-              if (!ok) f[q][h] = u32x4{0u, 0u, 0u, 0u};
-            } else {
-              f[q][h] = load_ragged(a.B, at, ok ? a.rank - s - 8 * g : 0, all);
-            }
+        for (int h = 0; h < 2; ++h) {
+          // row i of the product's 16 is column 8 (i / 4) + 4 h + i % 4 of the block
+          const int64_t col = n0 + 8 * ((lane & 15) >> 2) + 4 * h + (lane & 3);
+          const bool ok = (FULL || col < a.n) && s + 8 * g < a.rank;
+          const int64_t at = (base + col) * a.rank + s + 8 * g;
+          if constexpr (WHOLE) {
+            f[h] = *reinterpret_cast<const u32x4_a2*>(a.B + (ok ? at : 0));
+            if (!ok) f[h] = u32x4{0u, 0u, 0u, 0u};
+          } else {
+            f[h] = load_ragged(a.B, at, ok ? a.rank - s - 8 * g : 0, all);
           }
         }
       };
       if (mine) fetch(0);
-      f32x4 y[MT][NC][2];
+      const int64_t col = n0 + 8 * g;
+      f32x4 y[MT][2];
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int64_t r = row0 + 16 * i + (lane & 15);
         const float* c = a.C + (r < a.t ? r : a.t - 1) * a.n;
+        if constexpr (FULL) {              // (rows of other adapters too: they are not stored here)
+          y[i][0] = *reinterpret_cast<const f32x4_a4*>(c + col);
+          y[i][1] = *reinterpret_cast<const f32x4_a4*>(c + col + 4);
+        } else {
 #pragma unroll
-        for (int q = 0; q < NC; ++q) {
-          const int64_t col = n0 + 32 * q + 8 * g;
-          if constexpr (FULL) {            // (rows of other adapters too: they are not stored here)
-            y[i][q][0] = *reinterpret_cast<const f32x4_a4*>(c + col);
-            y[i][q][1] = *reinterpret_cast<const f32x4_a4*>(c + col + 4);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[i][q][e / 4][e % 4] = col + e < a.n ? c[col + e] : 0.0f;
-          }
+          for (int e = 0; e < 8; ++e) y[i][e / 4][e % 4] = col + e < a.n ? c[col + e] : 0.0f;
         }
       }
       if (mine) {
-        f32x4 acc[MT][NC][2];
+        f32x4 acc[MT][2];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-#pragma unroll
-          for (int q = 0; q < NC; ++q) acc[i][q][0] = acc[i][q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
+        for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         for (int s = 0; s < rp; s += 32) {
           if (s > 0) fetch(s);
 #pragma unroll
@@ -377,73 +368,62 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
             const u32x4 vh = *reinterpret_cast<const u32x4*>(hi + at);
             const u32x4 vl = *reinterpret_cast<const u32x4*>(lo + at);
 #pragma unroll
-            for (int q = 0; q < NC; ++q) {
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                acc[i][q][h] = mfma32<DT>(f[q][h], vl, acc[i][q][h]);
-                acc[i][q][h] = mfma32<DT>(f[q][h], vh, acc[i][q][h]);
-              }
+            for (int h = 0; h < 2; ++h) {
+              acc[i][h] = mfma32<DT>(f[h], vl, acc[i][h]);
+              acc[i][h] = mfma32<DT>(f[h], vh, acc[i][h]);
             }
           }
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
-          for (int q = 0; q < NC; ++q) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              y[i][q][0][e] = fmaf(acc[i][q][0][e], scale[i], y[i][q][0][e]);
-              y[i][q][1][e] = fmaf(acc[i][q][1][e], scale[i], y[i][q][1][e]);
-            }
+          for (int e = 0; e < 4; ++e) {
+            y[i][0][e] = fmaf(acc[i][0][e], scale[i], y[i][0][e]);
+            y[i][1][e] = fmaf(acc[i][1][e], scale[i], y[i][1][e]);
           }
         }
       } else if (which >= 0) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
-          for (int q = 0; q < NC; ++q) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[i][q][e / 4][e % 4] = __builtin_nanf("");
-          }
+          for (int e = 0; e < 8; ++e) y[i][e / 4][e % 4] = __builtin_nanf("");
         }
       }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         if (((mask >> (16 * i + (lane & 15))) & 1) == 0) continue;
         const int64_t o = (row0 + 16 * i + (lane & 15)) * a.n;
-#pragma unroll
-        for (int q = 0; q < NC; ++q) {
-          const int64_t col = n0 + 32 * q + 8 * g;
-          const f32x4 u = y[i][q][0], v = y[i][q][1];
-          if constexpr (HALF) {
-            auto* w = static_cast<uint16_t*>(a.Y) + o;
-            const u16x4 p = to_half4<DT>(u[0], u[1], u[2], u[3]), r = to_half4<DT>(v[0], v[1], v[2], v[3]);
-            if (FULL) {
-              const u32x2 pw = __builtin_bit_cast(u32x2, p), rw = __builtin_bit_cast(u32x2, r);
-              *reinterpret_cast<u32x4_a2*>(w + col) = u32x4{pw[0], pw[1], rw[0], rw[1]};
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                if (col + e < a.n) w[col + e] = e < 4 ? p[e] : r[e - 4];
-              }
-            }
+        const f32x4 u = y[i][0], v = y[i][1];
+        if constexpr (HALF) {
+          auto* w = static_cast<uint16_t*>(a.Y) + o;
+          const u16x4 p = to_half4<DT>(u[0], u[1], u[2], u[3]), r = to_half4<DT>(v[0], v[1], v[2], v[3]);
+          if (FULL) {
+            const u32x2 pw = __builtin_bit_cast(u32x2, p), rw = __builtin_bit_cast(u32x2, r);
+            *reinterpret_cast<u32x4_a2*>(w + col) = u32x4{pw[0], pw[1], rw[0], rw[1]};
           } else {
-            float* w = static_cast<float*>(a.Y) + o;
-            if (FULL) {
-              *reinterpret_cast<f32x4_a4*>(w + col) = u;
-              *reinterpret_cast<f32x4_a4*>(w + col + 4) = v;
-            } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                if (col + e < a.n) w[col + e] = e < 4 ? u[e] : v[e - 4];
-              }
+            for (int e = 0; e < 8; ++e) {
+              if (col + e < a.n) w[col + e] = e < 4 ? p[e] : r[e - 4];
+            }
+          }
+        } else {
+          float* w = static_cast<float*>(a.Y) + o;
+          if (FULL) {
+            *reinterpret_cast<f32x4_a4*>(w + col) = u;
+            *reinterpret_cast<f32x4_a4*>(w + col + 4) = v;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (col + e < a.n) w[col + e] = e < 4 ? u[e] : v[e - 4];
             }
           }
         }
       }
     };
-    for (int64_t n0 = c0 + wave * (32 * NC); n0 < c1; n0 += 128 * NC) {
-      if (n0 + 32 * NC <= a.n) {
+    // (a tile's work-groups walk its columns side by side; with a run of columns each, their lines of C
+    // lie far apart at any one time: 319 against 267 us at 8192 x 11008 with 28 blocks of columns each)
+    for (int64_t n0 = c0 + 32 * wave; n0 < a.n; n0 += int64_t{kColumns} * a.blocks) {
+      if (n0 + 32 <= a.n) {
         columns(n0, std::true_type{});
       } else {
         columns(n0, std::false_type{});
@@ -547,14 +527,14 @@ hipError_t launch_shrink(AdapterArgs a, const Plan& p, hipStream_t st) {
 
 template <int DT, int MT, bool HALF, bool WHOLE>
 hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
-  constexpr int NC = 1;
-  const auto kernel = expand_kernel<DT, MT, NC, HALF, WHOLE>;
-  // a work-group forms the tile's V once for all its columns: as many as leave three work-groups for
-  // every compute unit
-  const int64_t steps = (a.n + 128 * NC - 1) / (128 * NC);
-  const int64_t each = std::max<int64_t>(1, std::min<int64_t>(steps, a.tiles * steps / (3 * cus)));
-  a.cols = each * 128 * NC;
-  a.blocks = static_cast<int>((a.n + a.cols - 1) / a.cols);
+  const auto kernel = expand_kernel<DT, MT, HALF, WHOLE>;
+  // A work-group forms the tile's V once for all its columns: so many of them that three work-groups
+  // are left for every compute unit, but no more than the rank is worth, since later work-groups even
+  // out what is left at the end (8192 x 11008: rank 128 267 us without that bound, 211 us; rank 16 178
+  // and 146 us; with one block each rank 256 at 4096 x 4096 takes 139 us, not 118).
+  const int64_t steps = (a.n + kColumns - 1) / kColumns;
+  const int64_t each = std::max<int64_t>(1, std::min<int64_t>({steps, a.tiles * steps / (3 * cus), a.rank / 32}));
+  a.blocks = static_cast<int>((steps + each - 1) / each);
   a.ways = ways_of(MT, a.tiles * a.blocks, a.count, 4 * cus);
   const int rp = (a.rank + 31) / 32 * 32;
   const size_t lds = static_cast<size_t>(16 * MT) * (4 * (rp + 8) + 4 * rp + 4);
