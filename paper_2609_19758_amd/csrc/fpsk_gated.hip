@@ -720,14 +720,29 @@ hipError_t launch_grad(const uint16_t* dH, const float* P, int64_t t, int64_t f,
 
 // ---- host ------------------------------------------------------------------------------------
 
-// How a product is cut: tiles of 256 x 256 where they fill the chip, if need be with K in up to 4
-// parts of at least 32 steps; else of 128 x 128, with K in parts while those would not fill it twice
-// over and every part keeps at least 8 steps.
+// How a product is cut: tiles of 256 x 256 (one work-group a compute unit) or 128 x 128 (two), and K
+// in parts where the tiles alone would leave compute units idle.
 struct Cut {
   bool big, direct, few;
   int64_t tiles_m, tiles_n, kslice;
   int splits;
 };
+
+// Microseconds that a product of M x N takes in `tiles` tiles and `splits` parts of `per` steps, by
+// what the kernels measure: a step of 64 k takes 1.66 us in a tile of 256, 1.1 us in two of 128 side by
+// side and 0.6 us in one alone; a round of work-groups begins and ends in 5 and 3 us; operands come
+// from memory at 4.3 TB/s, 3.4 with a single tile of 128 per compute unit; and parts are written, read
+// and added at 5 TB/s in a launch of 3 us.  (4096 x 22016 x 4096: 667 us, measured 672; 500 x 22016 x
+// 4096: 111 and 110, where 256-tiles in two parts take 145 and 128-tiles 144; 1000 x 8192 x 4096: 73
+// and 67, in 256-tiles 79 in two parts, 93 in one; 67 x 27648 x 5120: 75 and 72, 86 in one part.)
+double cost(bool big, double M, double N, double K, int64_t tiles, int64_t splits, int64_t per, int cus) {
+  const int64_t groups = tiles * splits, slots = big ? cus : 2 * cus, rest = groups % slots;
+  const double steps = static_cast<double>(per), round = big ? 1.66 * steps + 5 : 1.1 * steps + 3;
+  double c = static_cast<double>(groups / slots) * round;
+  if (rest > 0) c += big || rest > cus ? round : 0.6 * steps + 3;
+  c = std::max(c, 2e-6 * K * (M + N) / (big || groups > cus ? 4.3 : 3.4));
+  return splits == 1 ? c : c + 3 + 8e-6 / 5 * static_cast<double>(splits) * M * N;
+}
 
 // cols: columns of the product, or of H (two of the product each).
 Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct, int cus) {
@@ -735,30 +750,30 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct
   c.direct = direct;
   c.big = false;
   c.few = few;
-  if (c.few) {
-    c.tiles_m = 1;
-    c.tiles_n = (cols + 15) / 16;
-    c.kslice = K;
-    c.splits = 1;
-    return c;
+  c.tiles_m = 1;
+  c.tiles_n = (cols + 15) / 16;
+  c.kslice = K;
+  c.splits = 1;
+  if (few) return c;
+  const int64_t steps = std::max<int64_t>(1, (K + kBK - 1) / kBK);
+  double best = -1.0;
+  for (const bool big : {true, false}) {
+    if (big && !direct) continue;
+    const int64_t edge = big ? 256 : 128, per_n = gated ? edge / 2 : edge;
+    const int64_t tm = (M + edge - 1) / edge, tn = (cols + per_n - 1) / per_n;
+    for (int64_t s = 1; s <= std::min<int64_t>(32, std::max<int64_t>(1, steps / 4)) && (s == 1 || tm * tn * (s - 1) < 2 * cus); ++s) {
+      const int64_t per = (steps + s - 1) / s, parts = (steps + per - 1) / per;
+      const double t = cost(big, static_cast<double>(M), static_cast<double>(gated ? 2 * cols : cols),
+                            static_cast<double>(K), tm * tn, parts, per, cus);
+      if (best >= 0.0 && t >= best) continue;
+      best = t;
+      c.big = big;
+      c.tiles_m = tm;
+      c.tiles_n = tn;
+      c.kslice = per * kBK;
+      c.splits = static_cast<int>(parts);
+    }
   }
-  auto tiles = [&](int edge) {
-    const int64_t per = gated ? edge / 2 : edge;
-    c.tiles_m = (M + edge - 1) / edge;
-    c.tiles_n = (cols + per - 1) / per;
-    return c.tiles_m * c.tiles_n;
-  };
-  const int64_t steps = (K + kBK - 1) / kBK, large = tiles(256);
-  int64_t s = large >= cus ? 1 : (cus + large - 1) / large;
-  c.big = direct && (large >= cus || (s <= 4 && steps >= 32 * s));
-  if (!c.big) {
-    const int64_t n = tiles(128);
-    s = n < 2 * cus ? std::min<int64_t>(2 * cus / n, steps / 8) : 1;
-  }
-  s = std::max<int64_t>(1, s);
-  const int64_t per = std::max<int64_t>(1, (steps + s - 1) / s);
-  c.kslice = per * kBK;
-  c.splits = static_cast<int>(std::max<int64_t>(1, (steps + per - 1) / per));
   return c;
 }
 
