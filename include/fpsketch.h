@@ -345,9 +345,9 @@ double fpsketch_rms_hat_samples(const float* samples, int64_t count);
 /* may be 0 and then NULL), aligned to 16 bytes; it belongs to the call until its work on      */
 /* `stream` is done, so calls that may overlap in time (other streams, graphs replayed beside  */
 /* each other) each need their own.  Sums, products and statistics are held in FP32 or more,   */
-/* and each result is rounded once.  FPSK_ESHAPE: a dimension outside [1, 2^31) (t: [0, 2^31)) */
-/* (gated block: d and 2f at most 2^22) or an array of more than 2^40 elements; FPSK_EINVAL: null or misaligned pointers and the    */
-/* rest.                                                                                       */
+/* and each result is rounded once.  FPSK_ESHAPE: a dimension outside [1, 2^31) (t: [0, 2^31); */
+/* gated block: d and 2f at most 2^22) or an array of more than 2^40 elements; FPSK_EINVAL:    */
+/* null or misaligned pointers and the rest.                                                   */
 
 typedef enum { FPSK_SILU = 0, FPSK_GELU = 1, FPSK_GELU_TANH = 2 } fpsketch_act;
 typedef enum { FPSK_PAIRS_HALF = 0, FPSK_PAIRS_INTERLEAVED = 1 } fpsketch_pairs;
@@ -400,7 +400,8 @@ int64_t fpsketch_adapters_workspace(int64_t t, int64_t k, int64_t n, int32_t cou
  * are normed with the gains gq, gk (hd FP32 each; both NULL: no norm),
  * x g / sqrt(mean x^2 + eps), then the first rd entries (even, at most hd) are rotated in pairs by
  * pos_i freq_p, p < rd / 2: pairs (p, p + rd / 2), or (2p, 2p + 1) with FPSK_PAIRS_INTERLEAVED.
- * Angles are formed and reduced in FP64.  pos and freq may be NULL when rd is 0. */
+ * Angles are formed and reduced in FP64; the squares are summed in FP32, so entries of normed heads
+ * stay below 2^59.  pos and freq may be NULL when rd is 0. */
 fpsketch_status fpsketch_heads(const float* C, int64_t t, int32_t hq, int32_t hkv, int32_t hd,
                                const float* gq, const float* gk, double eps, const int64_t* pos,
                                const float* freq, int32_t rd, int32_t pairs, fpsketch_dtype dtype,

@@ -25,7 +25,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # Matrix-core accumulators in ordinary VGPRs: with the compiler's default the loop-carried
 # accumulators of the FP64 bucket-space product were copied between VGPRs and AGPRs on every k-step
 # and the 64 x 64 product tile took 192 registers (2 waves per SIMD) instead of 98.  The digit
-# product's 224 accumulators belong in the AGPRs: in VGPRs they left 30 copies a step.
+# product's 224 accumulators belong in the AGPRs: in VGPRs they left 30 copies a step.  The gated
+# block's 256 x 256 tiles spill in that form.
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 NO_VGPR_FORM = {"fpsk_digits.hip", "fpsk_gated.hip"}
 

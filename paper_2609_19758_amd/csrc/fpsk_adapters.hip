@@ -32,10 +32,11 @@ struct AdapterArgs {
   int blocks;              // rank blocks (shrink), or work-groups that share a tile's columns (expand)
 };
 
-// Both kernels take tiles of neighbouring rows as they come, in turn over the adapters that a tile's rows name: an adapter's factor multiplies the whole tile on the matrix
-// cores, and only its own rows are kept.  The rows of a request are neighbours, so a prompt's tile
-// names one adapter or two and no sorting of rows is needed before; a decode tile names up to 16,
-// which `ways` work-groups take in turn.
+// Both kernels take tiles of neighbouring rows as they come, in turn over the adapters that a tile's
+// rows name: an adapter's factor multiplies the whole tile on the matrix cores, and only its own rows
+// are kept.  The rows of a request are neighbours, so a prompt's tile names one adapter or two and no
+// sorting of rows is needed before; a decode tile names up to 16, which `ways` work-groups take in turn
+// (48 tokens of 24 adapters: 15.7 us, 40.6 with one work-group to a tile).
 //
 // each(a, mask): a the adapter (-1: none, count: invalid), mask its rows in the tile.
 template <int TR, typename F>
@@ -92,7 +93,11 @@ __device__ __forceinline__ void shrink_store(const AdapterArgs& a, const ShrinkP
   }
 }
 
-// V = X A^T, both streamed through LDS; the parts of k are added by the next kernel, in order.
+// V = X A^T, both streamed through LDS; the parts of k are added by the next kernel, in order.  Bound
+// by reading X and by how few bytes of it the factor's rows leave room for under way: 4093 x 11008 at
+// rank 64 takes 39 us (2.3 TB/s of X), 31.8 us where every tile names one adapter; more parts of k or
+// two work-groups to every tile take longer (76.7 us for both kernels, 82 and 77).  48 x 4096 at rank
+// 16, 24 adapters: 6.1 us.
 template <int DT, int MT, int NT>
 __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, RB = 16 * NT, kBytes = WaveRows<MT>::kBytes + WaveRows<NT>::kBytes;
@@ -242,7 +247,8 @@ constexpr int kColumns = 128;   // of a work-group at a time, 32 per wave
 // and Y, whose loads and stores are whole lines: the columns of a 32-wide block are dealt to two
 // products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as two half
 // words, hi + lo, so that 16 (BF16) or 22 (FP16) of its bits count against the exact factor B; in
-// FP16 a row is first scaled by a power of two to where both words are in range.
+// FP16 a row is first scaled by a power of two to where both words are in range.  4093 x 4096 at rank
+// 64: 35 us, 2.8 TB/s; 48 x 4096 at rank 16, 24 adapters: 8.2 us.
 //
 // WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
 template <int DT, int MT, bool HALF, bool WHOLE>
@@ -463,8 +469,10 @@ __global__ __launch_bounds__(kThreads) void tiny_kernel(AdapterArgs a, int half)
 // ---- host ------------------------------------------------------------------------------------
 
 // How the work is cut: tiles of 32 rows in long batches (each factor is then read from L2 half as
-// often), of 16 in short ones; k in up to 8 parts while the tiles do not give every compute unit two
-// work-groups; and as many work-groups to a tile's adapters as that leaves room for.
+// often: 4093 tokens at rank 64 take 77 us, 103 in tiles of 16; 1500 at rank 16 22.4 and 23.9), of 16 in
+// short ones (48 tokens 15.7 us, 16.6 in tiles of 32); k in up to 8 parts while the tiles do not give
+// every compute unit two work-groups (4093 tokens without parts 81.5 us); and as many work-groups to a
+// tile's adapters as that leaves room for.
 struct Cut {
   int mt, ways;
   int64_t tiles;

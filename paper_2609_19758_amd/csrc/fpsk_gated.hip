@@ -12,6 +12,10 @@
 //   K-major (the product runs along the stored rows, W in dP W, both operands in dP^T X)
 //                              rows of one k, read with the transposing LDS read, which gives a
 //                              lane four k of one column: no operand is transposed in memory.
+// The activation's operands meet in one lane (gate and up rows take turns in a tile), so H is formed from
+// the accumulators while P is stored, and a verified block costs one pass over X, W, P and H.
+// 4096 x 4096 x 11008 BF16 (P and H): 670 us, 1.10 PFLOP/s; a library product alone takes 693 us there.
+// dX and dW at 2048 x 4096 x 11008: 685 us, 1.08 PFLOP/s (library products 355 and 319 us).
 #include "fpsk_layers.h"
 
 #include <algorithm>
@@ -125,9 +129,9 @@ struct Tile {
 
 // A stage: the same tile filled by loads that go straight to LDS: 16-byte groups on 16-byte
 // boundaries (rows a multiple of 8 long), 32-bit offsets within the tile (ld at most kMaxLd).  A
-// wave's 64 groups land in order, so the permutation is in the addresses.  Rows past the end repeat the last one, whose products
-// are not stored; for k past K the offset is one that the buffer's bounds turn into zeros.
-
+// wave's 64 groups land in order, so the permutation is in the addresses.  Rows past the end repeat
+// the last one, whose products are not stored; for k past K the offset is one that the buffer's
+// bounds turn into zeros.
 template <int R, int NT, bool KM, bool GATE>
 struct Stage {
   typedef Tile<R, NT, KM, GATE> T;
@@ -220,7 +224,8 @@ __device__ __forceinline__ void store4h(uint16_t* row, int64_t j, int64_t n, u16
 }
 
 // Work-groups are dealt to the 8 XCDs in turn; each XCD gets neighbouring tiles, in bands of 4 rows
-// of tiles, so that its L2 holds the operands' tiles that they share.
+// of tiles, so that its L2 holds the operands' tiles that they share (2048 x 16384 x 8192: bands of 8
+// rows 468 us, of 4 rows 448; 4096 x 22016 x 4096: 16 rows 717, 4 rows 661).
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
   const uint32_t per = tm * tn / 8;
   if (b < 8 * per) b = (b % 8) * per + b / 8;
@@ -333,7 +338,7 @@ struct Part {
 
 template <int BM, int BN, bool GATED>
 __device__ __forceinline__ Part part_of(const MmArgs& a, uint32_t block) {
-  // (32 bits: a launch has fewer work-groups, and a 64-bit division takes a microsecond)
+  // (32 bits: a launch has fewer work-groups, and 64-bit divisions are long)
   const auto rows = static_cast<uint32_t>(a.tiles_m), cols = static_cast<uint32_t>(a.tiles_n);
   const uint32_t split = block / (rows * cols);
   uint32_t tm, tn;
@@ -347,7 +352,8 @@ __device__ __forceinline__ Part part_of(const MmArgs& a, uint32_t block) {
   return p;
 }
 
-// Any alignment: the operands' tiles pass through registers.
+// Any alignment: the operands' tiles pass through registers, whose loads are two to four instructions a
+// group (worth_copies has the times of both kernels).
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mm_ragged_kernel(MmArgs a, int act) {
   typedef Wave<DT, BM, BN, WM, WN, AKM, BKM, GATED> W;
@@ -401,7 +407,10 @@ __device__ __forceinline__ void stages_ready() {
 
 // Whole 16-byte groups, two buffers of 64 k: the next step's loads are under way during this one's
 // products.  A buffer is an array of its own, so that the compiler knows loads into one apart from
-// reads of the other.
+// reads of the other.  Bound by the matrix cores: a step of a 256 x 256 tile takes 1.66 us, a rate of
+// 1.29 PFLOP/s (a library product of 8192 x 8192 x 8192 reaches 1.23 to FP32).  At 4096 x 22016 x 4096,
+// loads spread between the products take longer (670 -> 735 us), as do non-temporal stores (674 -> 680)
+// and tiles of the last round in halves (667 -> 676).
 template <int DT, int BM, int BN, int WM, int WN, bool AKM, bool BKM, bool GATED>
 __device__ __forceinline__ void mm_tile(const MmArgs& a, int act, uint32_t block, char* a0, char* b0,
                                         char* a1, char* b1) {
@@ -462,6 +471,8 @@ __global__ __launch_bounds__(256, 2) void mm_pair_kernel(MmArgs dx, MmArgs dw, u
 
 // Up to 16 tokens: bound by reading W once.  A work-group takes 16 columns of H and all tokens; each
 // wave streams a run of k of its gate rows, up rows and tokens, and the waves' sums meet in LDS.
+// 1 x 4096 x 11008: 32.4 us, 5.6 TB/s of W; 16 tokens: 36 us, 48 us in mm_kernel, which keeps fewer
+// bytes under way (17 tokens: 48 us).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void few_kernel(MmArgs a, int act) {
   constexpr int kWaves = kThreads / 64, kBytes = WaveRows<1>::kBytes + WaveRows<2>::kBytes;
@@ -603,7 +614,8 @@ __global__ __launch_bounds__(kThreads) void mm_sum_kernel(MmArgs a, int act) {
   }
 }
 
-// H = act(G) U from a delivered product, one element a thread.
+// H = act(G) U from a delivered product, one element a thread: bound by reading P and writing H (2048 x
+// 11008: 45.8 us, 4.9 TB/s of a copy's 5.15).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void narrow_kernel(const float* P, int64_t t, int64_t f,
                                                           int act, uint16_t* H) {
@@ -623,7 +635,9 @@ __device__ __forceinline__ void grads(float g, float u, float dh, float* dg, flo
 
 // dP of a 64 x 64 block of H: bound by its loads and stores (14 bytes an entry of H, 18 with the
 // transpose).  A thread takes 4 x 4 entries, all loads at once, and turns them in registers for the
-// transpose, whose rows then leave LDS as whole lines.
+// transpose, whose rows then leave LDS as whole lines.  2048 x 11008 with the transpose: 84.6 us, 4.8
+// TB/s of a copy's 5.15; 1531 x 13824, whose transposed rows begin inside lines: 88 us, 4.3 TB/s
+// (blocks of 128 tokens: 93 us).
 template <int DT, int ACT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, const float* P, int64_t t,
                                                         int64_t f, uint16_t* dP, uint16_t* dPt,
