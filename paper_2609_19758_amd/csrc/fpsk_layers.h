@@ -17,10 +17,6 @@ fpsketch_status layer_error(fpsketch_status s, const char* detail) noexcept;
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef u16x4 u16x4_a2 __attribute__((aligned(2)));
-typedef u16x2 u16x2_a2 __attribute__((aligned(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef f32x2 f32x2_a4 __attribute__((aligned(4)));
-typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
