@@ -775,7 +775,9 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct
     if (big && !direct) continue;
     const int64_t edge = big ? 256 : 128, per_n = gated ? edge / 2 : edge;
     const int64_t tm = (M + edge - 1) / edge, tn = (cols + per_n - 1) / per_n;
-    for (int64_t s = 1; s <= std::min<int64_t>(32, std::max<int64_t>(1, steps / 4)) && (s == 1 || tm * tn * (s - 1) < 2 * cus); ++s) {
+    // up to 32 parts of at least 4 steps, while those before leave compute units free
+    const int64_t most = std::min<int64_t>({32, std::max<int64_t>(1, steps / 4), 1 + 2 * cus / (tm * tn)});
+    for (int64_t s = 1; s <= most; ++s) {
       const int64_t per = (steps + s - 1) / s, parts = (steps + per - 1) / per;
       const double t = cost(big, static_cast<double>(M), static_cast<double>(gated ? 2 * cols : cols),
                             static_cast<double>(K), tm * tn, parts, per, cus);
