@@ -223,12 +223,17 @@ __device__ __forceinline__ void store4h(uint16_t* row, int64_t j, int64_t n, u16
   }
 }
 
-// Work-groups are dealt to the 8 XCDs in turn; each XCD gets neighbouring tiles, in bands of 4 rows
+// Work-groups are dealt to the 8 XCDs in turn: with this order each XCD gets neighbours among `count`.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t b, uint32_t count) {
+  const uint32_t per = count / 8;
+  return b < 8 * per ? (b % 8) * per + b / 8 : b;
+}
+
+// Each XCD gets neighbouring tiles, in bands of 4 rows
 // of tiles, so that its L2 holds the operands' tiles that they share (2048 x 16384 x 8192: bands of 8
 // rows 468 us, of 4 rows 448; 4096 x 22016 x 4096: 16 rows 717, 4 rows 661).
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t tm, uint32_t tn, uint32_t* m, uint32_t* n) {
-  const uint32_t per = tm * tn / 8;
-  if (b < 8 * per) b = (b % 8) * per + b / 8;
+  b = by_xcd(b, tm * tn);
   const uint32_t band = b / (4 * tn), first = 4 * band;
   const uint32_t height = tm - first < 4 ? tm - first : 4;
   const uint32_t in = b - band * 4 * tn;
@@ -635,24 +640,30 @@ __device__ __forceinline__ void grads(float g, float u, float dh, float* dg, flo
 
 // dP of a 64 x 64 block of H: bound by its loads and stores (14 bytes an entry of H, 18 with the
 // transpose).  A thread takes 4 x 4 entries, all loads at once, and turns them in registers for the
-// transpose, whose rows then leave LDS as whole lines.  2048 x 11008 with the transpose: 84.6 us, 4.8
-// TB/s of a copy's 5.15; 1531 x 13824, whose transposed rows begin inside lines: 88 us, 4.3 TB/s
-// (blocks of 128 tokens: 93 us).
+// transpose, whose rows then leave LDS as whole lines.  2048 x 11008 with the transpose: 84 us, 4.8
+// TB/s of a copy's 5.15; 1531 x 13824, whose transposed rows begin inside lines: 83 us, 4.6 TB/s (without
+// the transpose 56 us, 5.3 TB/s).  Strips of tokens whose lines meet in LDS are no faster (99 us), nor
+// blocks of 128 tokens (105).
+//
+// Blocks are taken in bands of `band` columns of blocks, down a band; xcd: neighbours on one XCD.
 template <int DT, int ACT>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, const float* P, int64_t t,
                                                         int64_t f, uint16_t* dP, uint16_t* dPt,
-                                                        int64_t blocks_f) {
+                                                        uint32_t blocks_t, uint32_t band, bool xcd) {
   constexpr int kEdge = 64;
   __shared__ __attribute__((aligned(16))) uint16_t tile[2][kEdge][kEdge + 4];   // columns x tokens
-  const int64_t m0 = (blockIdx.x / blocks_f) * kEdge, j0 = (blockIdx.x % blocks_f) * kEdge;
+  const uint32_t blocks_f = gridDim.x / blocks_t, b = xcd ? by_xcd(blockIdx.x, gridDim.x) : blockIdx.x;
+  const uint32_t first = b / (band * blocks_t) * band, width = blocks_f - first < band ? blocks_f - first : band;
+  const uint32_t in = b - first * blocks_t, m = in / width;
+  const int64_t m0 = static_cast<int64_t>(m) * kEdge, j0 = static_cast<int64_t>(first + in - m * width) * kEdge;
   const int x = 4 * (threadIdx.x & 15), y = 4 * (threadIdx.x >> 4);
-  const bool full = m0 + kEdge <= t && j0 + kEdge <= f;
+  const bool whole = j0 + x + 3 < f;       // (tokens past the last one: that one again, not stored)
   f32x4 g[4], u[4];
   u16x4 h[4];
-  if (full) {
+  if (whole) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t m = m0 + y + r, at = 2 * m * f + j0 + x;
+      const int64_t m = m0 + y + r < t ? m0 + y + r : t - 1, at = 2 * m * f + j0 + x;
       g[r] = *reinterpret_cast<const f32x4_a4*>(P + at);
       u[r] = *reinterpret_cast<const f32x4_a4*>(P + at + f);
       h[r] = *reinterpret_cast<const u16x4_a2*>(dH + m * f + j0 + x);
@@ -662,11 +673,10 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, cons
     for (int r = 0; r < 4; ++r) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int64_t m = m0 + y + r, j = j0 + x + e;
-        const bool in = m < t && j < f;
-        g[r][e] = in ? P[2 * m * f + j] : 0.0f;
-        u[r][e] = in ? P[2 * m * f + f + j] : 0.0f;
-        h[r][e] = in ? dH[m * f + j] : uint16_t{0};
+        const int64_t m = m0 + y + r < t ? m0 + y + r : t - 1, j = j0 + x + e;
+        g[r][e] = j < f ? P[2 * m * f + j] : 0.0f;
+        u[r][e] = j < f ? P[2 * m * f + f + j] : 0.0f;
+        h[r][e] = j < f ? dH[m * f + j] : uint16_t{0};
       }
     }
   }
@@ -684,13 +694,14 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, cons
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int64_t m = m0 + y + r, at = 2 * m * f + j0 + x;
-    if (full) {
+    if (m >= t) continue;
+    if (whole) {
       *reinterpret_cast<u16x4_a2*>(dP + at) = hg[r];
       *reinterpret_cast<u16x4_a2*>(dP + at + f) = hu[r];
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (m < t && j0 + x + e < f) {
+        if (j0 + x + e < f) {
           dP[at + e] = hg[r][e];
           dP[at + f + e] = hu[r][e];
         }
@@ -709,10 +720,11 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, cons
     const int half = i & 1, c = (threadIdx.x >> 4) + 16 * (i >> 1);
     const u16x4 v = *reinterpret_cast<const u16x4*>(&tile[half][c][x]);
     const int64_t j = j0 + c, m = m0 + x;
+    if (j >= f) continue;
     uint16_t* to = dPt + (j + half * f) * t + m;
-    if (full) {
+    if (m + 3 < t) {
       *reinterpret_cast<u16x4_a2*>(to) = v;
-    } else if (j < f) {
+    } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (m + e < t) to[e] = v[e];
@@ -724,11 +736,17 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const uint16_t* dH, cons
 template <int DT>
 hipError_t launch_grad(const uint16_t* dH, const float* P, int64_t t, int64_t f, int act, uint16_t* dP,
                        uint16_t* dPt, hipStream_t st) {
-  const int64_t bf = (f + 63) / 64;
-  const dim3 grid(static_cast<unsigned>(bf * ((t + 63) / 64)));
-  if (act == FPSK_SILU) FPSK_LAUNCH((grad_kernel<DT, 0>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bf);
-  if (act == FPSK_GELU) FPSK_LAUNCH((grad_kernel<DT, 1>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bf);
-  if (act == FPSK_GELU_TANH) FPSK_LAUNCH((grad_kernel<DT, 2>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bf);
+  const auto bt = static_cast<uint32_t>((t + 63) / 64), bf = static_cast<uint32_t>((f + 63) / 64);
+  const bool odd_t = dPt != nullptr && (t % 64 != 0 || !aligned(dPt, 128)), odd_f = f % 64 != 0 || !aligned(dP, 128);
+  // Where rows do not begin on 128-byte lines, neighbours share lines, which are written once if they meet in
+  // one L2: columns of blocks one after the other per XCD for the transpose's rows (1531 x 13824: 99 us in
+  // rows of blocks, 83), rows of blocks for dP's (1024 x 13001: 67 and 55), bands of 8 columns for both
+  // (1000 x 13001: 79 and 61).  On lines, rows of blocks over all XCDs (1536 x 13824: 76, 80 in columns).
+  const uint32_t band = odd_t ? (odd_f ? 8 : 1) : bf;
+  const dim3 grid(bf * bt);
+  if (act == FPSK_SILU) FPSK_LAUNCH((grad_kernel<DT, 0>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bt, band, odd_t || odd_f);
+  if (act == FPSK_GELU) FPSK_LAUNCH((grad_kernel<DT, 1>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bt, band, odd_t || odd_f);
+  if (act == FPSK_GELU_TANH) FPSK_LAUNCH((grad_kernel<DT, 2>), grid, dim3(kThreads), 0, st, dH, P, t, f, dP, dPt, bt, band, odd_t || odd_f);
   return hipSuccess;
 }
 

@@ -114,6 +114,25 @@ def test_long_batches_of_the_widest_adapters(fl, rank, fmt):
         assert torch.equal(out, Y)
 
 
+@pytest.mark.parametrize("fmt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("t,f,shift", [(1531, 8200, 0), (451, 16400, 1), (1600, 8192, 0), (1600, 8192, 5), (256, 129, 3),
+                                       (1023, 64, 0), (2177, 12345, 33), (257, 50000, 0)])
+def test_long_gradients_and_their_transposes(fl, t, f, shift, fmt):
+    """Rows of the gradient and of its transpose that begin on lines and inside them: the gradient is the one
+    without a transpose, and nothing beside either buffer is written."""
+    g = gen(t + f)
+    dH, P = gauss(g, t, f, std=0.5, to=fmt), gauss(g, t, 2 * f)
+    want, _ = fl.gated_grad(dH, P, act="gelu")
+    n = 2 * t * f
+    bufs = [torch.full((shift + n + 70,), 7.0, dtype=fmt, device="cuda") for _ in range(2)]
+    dP, dPt = bufs[0][shift:shift + n].view(t, 2 * f), bufs[1][shift:shift + n].view(2 * f, t)
+    fl.gated_grad(dH, P, act="gelu", transpose=True, dP=dP, dPt=dPt)
+    assert torch.equal(dP, want)
+    assert torch.equal(dPt, want.t())
+    for b in bufs:
+        assert bool((b[:shift] == 7).all()) and bool((b[shift + n:] == 7).all())
+
+
 # ---- with the verifier ---------------------------------------------------------------------
 
 
