@@ -316,6 +316,9 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           h[e] = to_half<DT>(s[e]);
+          // (BF16: a finite sum that would round to infinity keeps the largest number as its first word,
+          // and what is left as its second)
+          if (DT == 1 && (h[e] & 0x7fffu) == 0x7f80u && fabsf(s[e]) < __builtin_inff()) h[e] -= 1;
           const float rest = s[e] - from_half<DT>(h[e]);
           l[e] = fabsf(s[e]) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
         }

@@ -1,0 +1,41 @@
+"""How the rank sums V = X A^T of `adapters` reach the second product.  V is held in FP32, so whatever it
+is, Y is what FP32's V gives: the entries here make every step exact (small integers times powers of two,
+one term a sum), and Y is compared for equality."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def fl():
+    assert torch.cuda.is_available()
+    from paper_2609_19758_amd import fpsketch, layers
+    fpsketch.load()
+    return layers
+
+
+def call(fl, C, X, A, B, index, scale):
+    return fl.adapters(*[x.cuda() for x in (C, X, A, B, index, scale)], out="f32").cpu()
+
+
+@pytest.mark.parametrize("t", [5, 1030])
+@pytest.mark.parametrize("rank", [8, 13])
+def test_rank_sums_next_to_overflow(fl, t, rank):
+    """A sum above BF16's largest number and below FP32's."""
+    k, n = 64, 70
+    h = torch.bfloat16
+    X, A = torch.zeros(t, k, dtype=h), torch.zeros(1, rank, k, dtype=h)
+    top = 1.9921875 * 2.0 ** 63
+    X[:, :3] = torch.tensor([top, 2.0 ** 63, 2.0 ** 62])
+    X[1::2] *= -1
+    A[0, 2, :3] = torch.tensor([top, 2.0 ** 57, 2.0 ** 57])
+    V = X[:, :3].double() @ A[0, 2, :3].double()
+    assert bool(torch.isinf(V.to(h)).all()) and bool(torch.isfinite(V.float()).all())
+    B = torch.zeros(1, n, rank, dtype=h)
+    B[0, :, 2] = torch.pow(2.0, -(torch.arange(n) % 9).double()).to(h)
+    Y = call(fl, torch.zeros(t, n), X, A, B, torch.zeros(t, dtype=torch.int32), torch.tensor([2.0 ** -10]))
+    want = V[:, None] * B[0, :, 2].double() * 2.0 ** -10
+    assert torch.equal(Y.double(), want)
