@@ -295,7 +295,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (!own || c + e >= a.rank) sum[e] = 0.0f;
-          top = fmaxf(top, fabsf(sum[e]));
+          if (fabsf(sum[e]) < __builtin_inff()) top = fmaxf(top, fabsf(sum[e]));
         }
         *reinterpret_cast<f32x4*>(sums + r * rp + c) = sum;
       }
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
       if constexpr (DT == 0) {
 #pragma unroll
         for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, PER));
-        if (top > 0.0f && top < __builtin_inff()) {
+        if (top > 0.0f) {                  // (of the finite ones: they stay in range beside an infinite one)
           int e = ilogbf(top);
           e = e < -126 ? -126 : (e > 126 ? 126 : e);
           up = ldexpf(1.0f, -e);

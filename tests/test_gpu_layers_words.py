@@ -39,3 +39,19 @@ def test_rank_sums_next_to_overflow(fl, t, rank):
     Y = call(fl, torch.zeros(t, n), X, A, B, torch.zeros(t, dtype=torch.int32), torch.tensor([2.0 ** -10]))
     want = V[:, None] * B[0, :, 2].double() * 2.0 ** -10
     assert torch.equal(Y.double(), want)
+
+
+@pytest.mark.parametrize("t", [5, 1030])
+def test_large_rank_sums_beside_an_infinite_one(fl, t):
+    """FP16: an infinite sum beside a finite one beyond FP16's range.  Y is infinite with the sign of the
+    infinite term; the finite one must not turn it into NaN."""
+    k, n, rank = 64, 40, 8
+    h = torch.float16
+    X, A, B = torch.zeros(t, k, dtype=h), torch.zeros(1, rank, k, dtype=h), torch.zeros(1, n, rank, dtype=h)
+    X[:, 0], X[:, 1] = 1.0, 1000.0
+    A[0, 0, 0], A[0, 3, 1] = float("inf"), 1000.0
+    A[0, 0, 1] = 1.0
+    B[0, :, 0] = torch.where(torch.arange(n) % 2 == 0, 1.0, -2.0).to(h)
+    B[0, :, 3] = 1.0
+    Y = call(fl, torch.zeros(t, n), X, A, B, torch.zeros(t, dtype=torch.int32), torch.ones(1))
+    assert torch.equal(Y, torch.where(torch.arange(n) % 2 == 0, float("inf"), -float("inf")).expand(t, n))
