@@ -243,23 +243,40 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_ragged_kernel(Adapte
 
 constexpr int kColumns = 128;   // of a work-group at a time, 32 per wave
 
+// A rank sum as half words, whose sum it is: in BF16 three of 8 bits, all 24 that it has; in FP16 two of 11.
+template <int DT>
+constexpr int kWords = DT == 1 ? 3 : 2;
+
+template <int DT>
+__device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords<DT>]) {
+  w[0] = to_half<DT>(s);
+  const bool finite = fabsf(s) < __builtin_inff();
+  // (BF16: a finite sum that would round to infinity keeps the largest number as its first word)
+  if (DT == 1 && (w[0] & 0x7fffu) == 0x7f80u && finite) w[0] -= 1;
+  float rest = s - from_half<DT>(w[0]);    // (exact, as is each one after it)
+#pragma unroll
+  for (int i = 1; i < kWords<DT>; ++i) {
+    w[i] = finite ? to_half<DT>(rest) : uint16_t{0};
+    rest -= from_half<DT>(w[i]);
+  }
+}
+
 // Y = C + s V B^T on a tile of 16 MT rows.  Bound by C
 // and Y, whose loads and stores are whole lines: the columns of a 32-wide block are dealt to two
-// products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as two half
-// words, hi + lo, so that 16 (BF16) or 22 (FP16) of its bits count against the exact factor B; in
-// FP16 a row is first scaled by a power of two to where both words are in range.  4093 x 4096 at rank
-// 64: 35 us, 2.8 TB/s; 48 x 4096 at rank 16, 24 adapters: 8.2 us.
+// products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as half words
+// (split_words) against the exact factor B; in FP16 a row is first scaled by a power of two to where its
+// words are in range.  4093 x 4096 at rank 64: 36 us, 2.8 TB/s; 48 x 4096 at rank 16, 24 adapters, in BF16:
+// 8.9 us (8.5 with two words; 202 and 197 at 8192 x 11008, rank 128).
 //
 // WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
 template <int DT, int MT, bool HALF, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, PER = kThreads / TR;      // threads per row of V
+  constexpr int W = kWords<DT>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int rp = (a.rank + 31) / 32 * 32, ld = rp + 8;  // ranks as the products take them
-  uint16_t* hi = reinterpret_cast<uint16_t*>(smem);     // TR x ld
-  uint16_t* lo = hi + TR * ld;
-  float* sums = reinterpret_cast<float*>(lo + TR * ld); // TR x rp
-  float* back = sums + TR * rp;                         // TR: what undoes the scaling
+  uint16_t* words = reinterpret_cast<uint16_t*>(smem);  // W x TR x ld
+  float* back = reinterpret_cast<float*>(words + W * TR * ld);   // TR: what undoes the scaling
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   unsigned b = blockIdx.x;
   const int64_t c0 = static_cast<int64_t>(b % a.blocks) * kColumns;
@@ -278,6 +295,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
       const int r = threadIdx.x / PER, p = threadIdx.x % PER;
       const bool own = ((mask >> r) & 1) != 0;
       const float* v = a.V + (own ? row0 + r : row0) * a.ldv;
+      uint16_t *first = words + r * ld, *second = first + TR * ld;
       const int64_t part = a.t * a.ldv;
       float top = 0.0f;
 #pragma unroll 2
@@ -297,7 +315,10 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
           if (!own || c + e >= a.rank) sum[e] = 0.0f;
           if (fabsf(sum[e]) < __builtin_inff()) top = fmaxf(top, fabsf(sum[e]));
         }
-        *reinterpret_cast<f32x4*>(sums + r * rp + c) = sum;
+        // (until the row's scale is known, the two halves of its bits in the places of its first words)
+        const u32x4 bits = __builtin_bit_cast(u32x4, sum);
+        *reinterpret_cast<u16x4*>(first + c) = __builtin_convertvector(bits >> 16, u16x4);
+        *reinterpret_cast<u16x4*>(second + c) = __builtin_convertvector(bits & 0xffffu, u16x4);
       }
       float up = 1.0f, down = 1.0f;
       if constexpr (DT == 0) {
@@ -311,19 +332,17 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
         }
       }
       for (int c = 4 * p; c < rp; c += 4 * PER) {
-        const f32x4 s = *reinterpret_cast<const f32x4*>(sums + r * rp + c) * up;
-        u16x4 h, l;
+        const u16x4 top16 = *reinterpret_cast<const u16x4*>(first + c), low16 = *reinterpret_cast<const u16x4*>(second + c);
+        u16x4 word[W];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          h[e] = to_half<DT>(s[e]);
-          // (BF16: a finite sum that would round to infinity keeps the largest number as its first word,
-          // and what is left as its second)
-          if (DT == 1 && (h[e] & 0x7fffu) == 0x7f80u && fabsf(s[e]) < __builtin_inff()) h[e] -= 1;
-          const float rest = s[e] - from_half<DT>(h[e]);
-          l[e] = fabsf(s[e]) < __builtin_inff() ? to_half<DT>(rest) : uint16_t{0};
+          uint16_t w[W];
+          split_words<DT>(__uint_as_float(static_cast<uint32_t>(top16[e]) << 16 | low16[e]) * up, w);
+#pragma unroll
+          for (int i = 0; i < W; ++i) word[i][e] = w[i];
         }
-        *reinterpret_cast<u16x4*>(hi + r * ld + c) = h;
-        *reinterpret_cast<u16x4*>(lo + r * ld + c) = l;
+#pragma unroll
+        for (int i = 0; i < W; ++i) *reinterpret_cast<u16x4*>(first + i * TR * ld + c) = word[i];
       }
       if (p == 0) back[r] = down;
       __syncthreads();
@@ -374,12 +393,11 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             const int at = (16 * i + (lane & 15)) * ld + s + 8 * g;
-            const u32x4 vh = *reinterpret_cast<const u32x4*>(hi + at);
-            const u32x4 vl = *reinterpret_cast<const u32x4*>(lo + at);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              acc[i][h] = mfma32<DT>(f[h], vl, acc[i][h]);
-              acc[i][h] = mfma32<DT>(f[h], vh, acc[i][h]);
+            for (int w = W - 1; w >= 0; --w) {
+              const u32x4 v = *reinterpret_cast<const u32x4*>(words + w * TR * ld + at);
+              acc[i][0] = mfma32<DT>(f[0], v, acc[i][0]);
+              acc[i][1] = mfma32<DT>(f[1], v, acc[i][1]);
             }
           }
         }
@@ -548,13 +566,8 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
   a.blocks = static_cast<int>((steps + each - 1) / each);
   a.ways = ways_of(MT, a.tiles * a.blocks, a.count, 4 * cus);
   const int rp = (a.rank + 31) / 32 * 32;
-  const size_t lds = static_cast<size_t>(16 * MT) * (4 * (rp + 8) + 4 * rp + 4);
+  const size_t lds = static_cast<size_t>(16 * MT) * (2 * kWords<DT> * (rp + 8) + 4);   // (at most 50816 bytes)
   const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks)), block(kThreads);
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-    if (e != hipSuccess) return e;
-  }
   FPSK_LAUNCH(kernel, grid, block, lds, st, a);
   return hipSuccess;
 }

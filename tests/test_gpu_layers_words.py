@@ -55,3 +55,42 @@ def test_large_rank_sums_beside_an_infinite_one(fl, t):
     B[0, :, 3] = 1.0
     Y = call(fl, torch.zeros(t, n), X, A, B, torch.zeros(t, dtype=torch.int32), torch.ones(1))
     assert torch.equal(Y, torch.where(torch.arange(n) % 2 == 0, float("inf"), -float("inf")).expand(t, n))
+
+
+def digits(t, rank, fmt, seed):
+    """X, A and the sums V = X A^T (float64): three 8-bit digits of X to a sum of up to 24 bits, the ranks
+    2^7 apart in size, some of them with fewer digits."""
+    g = torch.Generator().manual_seed(seed)
+    k, h = 64, HALF[fmt]
+    X = torch.zeros(t, k)
+    A = torch.zeros(1, rank, k)
+    X[:, :48] = torch.randint(-255, 256, (t, 48), generator=g).float()
+    for e in range(rank):
+        at = 3 * (e % 16)
+        place = torch.tensor([1.0, 2.0 ** 8, 2.0 ** (16 if fmt == "bf16" else 15)])
+        place[3 - e // 16 % 3:] = 0.0                    # ranks from 16 on: two digits, then one
+        A[0, e, at:at + 3] = place * 2.0 ** (-7 * (e % 3))
+    V = X.double() @ A[0].double().t()
+    assert torch.equal(V.float().double(), V)
+    assert torch.equal(X.to(h).float(), X) and torch.equal(A.to(h).float(), A)
+    return X.to(h), A.to(h), V
+
+
+@pytest.mark.parametrize("t", [20, 1100])
+@pytest.mark.parametrize("rank", [3, 8, 31, 64, 256])
+@pytest.mark.parametrize("fmt", ["bf16"])
+def test_every_bit_of_the_rank_sums(fl, t, rank, fmt):
+    """Column j takes sum j % rank alone."""
+    X, A, V = digits(t, rank, fmt, t + rank)
+    n = max(rank + 5, 130)
+    B = torch.zeros(1, n, rank, dtype=HALF[fmt])
+    j = torch.arange(n)
+    B[0, j, j % rank] = torch.where(j % 2 == 0, 1.0, -0.25).to(HALF[fmt])
+    index = torch.zeros(t, dtype=torch.int32)
+    index[::7] = -1
+    C = torch.zeros(t, n)
+    C[::7] = 5.0
+    Y = call(fl, C, X, A, B, index, torch.tensor([2.0]))
+    want = 2.0 * V[:, j % rank] * B[0, j, j % rank].double()
+    want[::7] = 5.0
+    assert torch.equal(Y.double(), want)
