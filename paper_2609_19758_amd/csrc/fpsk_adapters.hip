@@ -243,19 +243,22 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_ragged_kernel(Adapte
 
 constexpr int kColumns = 128;   // of a work-group at a time, 32 per wave
 
-// A rank sum as half words, whose sum it is: in BF16 three of 8 bits, all 24 that it has; in FP16 two of 11.
-template <int DT>
-constexpr int kWords = DT == 1 ? 3 : 2;
+// A rank sum in three half words, whose sum it is with all of its 24 bits: 8 each in BF16; in FP16 11
+// each, the later two 2^12 times as large, so that they are in FP16's range wherever the first is (sums are
+// scaled to below 2^15 before).
+constexpr int kWords = 3;
+constexpr float kLater = 4096.0f;
 
 template <int DT>
-__device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords<DT>]) {
+__device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords]) {
   w[0] = to_half<DT>(s);
   const bool finite = fabsf(s) < __builtin_inff();
   // (BF16: a finite sum that would round to infinity keeps the largest number as its first word)
   if (DT == 1 && (w[0] & 0x7fffu) == 0x7f80u && finite) w[0] -= 1;
   float rest = s - from_half<DT>(w[0]);    // (exact, as is each one after it)
+  if constexpr (DT == 0) rest *= kLater;
 #pragma unroll
-  for (int i = 1; i < kWords<DT>; ++i) {
+  for (int i = 1; i < kWords; ++i) {
     w[i] = finite ? to_half<DT>(rest) : uint16_t{0};
     rest -= from_half<DT>(w[i]);
   }
@@ -264,15 +267,16 @@ __device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords<DT>]) 
 // Y = C + s V B^T on a tile of 16 MT rows.  Bound by C
 // and Y, whose loads and stores are whole lines: the columns of a 32-wide block are dealt to two
 // products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as half words
-// (split_words) against the exact factor B; in FP16 a row is first scaled by a power of two to where its
-// words are in range.  4093 x 4096 at rank 64: 36 us, 2.8 TB/s; 48 x 4096 at rank 16, 24 adapters, in BF16:
-// 8.9 us (8.5 with two words; 202 and 197 at 8192 x 11008, rank 128).
+// (split_words) against the exact factor B; in FP16 a row is first scaled by a power of two that puts its
+// largest sum at 2^14, and its later words have sums of their own.  4093 x 4096 at rank 64 in FP16: 36.4 us,
+// 2.8 TB/s (36.3 with two words, which lose bits; 8192 x 11008 at rank 128 205 and 198, 4096 x 4096 at rank 256 87
+// and 79); 48 x 4096 at rank 16, 24 adapters, in BF16: 8.9 us (8.7).
 //
 // WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
 template <int DT, int MT, bool HALF, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, PER = kThreads / TR;      // threads per row of V
-  constexpr int W = kWords<DT>;
+  constexpr int W = kWords;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int rp = (a.rank + 31) / 32 * 32, ld = rp + 8;  // ranks as the products take them
   uint16_t* words = reinterpret_cast<uint16_t*>(smem);  // W x TR x ld
@@ -287,9 +291,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
   for_adapters<TR>(a, row0, way, [&](int which, uint64_t mask) {
     const bool mine = which >= 0 && which < a.count;
     const int64_t base = static_cast<int64_t>(which) * a.n, all = static_cast<int64_t>(a.count) * a.n * a.rank;
-    float scale[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) scale[i] = 0.0f;
+    float scale = 0.0f, undo[MT] = {};
     if (mine) {
       __syncthreads();                     // the V of the adapter before
       const int r = threadIdx.x / PER, p = threadIdx.x % PER;
@@ -325,8 +327,8 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
 #pragma unroll
         for (int o = PER / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, PER));
         if (top > 0.0f) {                  // (of the finite ones: they stay in range beside an infinite one)
-          int e = ilogbf(top);
-          e = e < -126 ? -126 : (e > 126 ? 126 : e);
+          int e = ilogbf(top) - 14;
+          e = e < -126 ? -126 : e;
           up = ldexpf(1.0f, -e);
           down = ldexpf(1.0f, e);
         }
@@ -346,8 +348,9 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
       }
       if (p == 0) back[r] = down;
       __syncthreads();
+      scale = a.scale[which];
 #pragma unroll
-      for (int i = 0; i < MT; ++i) scale[i] = a.scale[which] * back[16 * i + (lane & 15)];
+      for (int i = 0; i < MT; ++i) undo[i] = back[16 * i + (lane & 15)];
     }
 
     // FULL: the wave's 32 columns all lie in the row.
@@ -385,28 +388,41 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
         }
       }
       if (mine) {
-        f32x4 acc[MT][2];
+        // FP16's later words: summed over all ranks in one row of blocks, per 32 ranks in two (over all of them
+        // 4093 x 4096 takes 72 registers and 40 us, not 64 and 36; 48 tokens take 8.9 us, per 32 ranks 10.4)
+        f32x4 acc[MT][2] = {}, later[2] = {};
+        auto add_later = [&](int i) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int e = 0; e < 8; ++e) {
+            acc[i][e / 4][e % 4] = fmaf(later[e / 4][e % 4], 1.0f / kLater, acc[i][e / 4][e % 4]);
+          }
+        };
         for (int s = 0; s < rp; s += 32) {
           if (s > 0) fetch(s);
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             const int at = (16 * i + (lane & 15)) * ld + s + 8 * g;
+            if constexpr (MT > 1) later[0] = later[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = W - 1; w >= 0; --w) {
               const u32x4 v = *reinterpret_cast<const u32x4*>(words + w * TR * ld + at);
-              acc[i][0] = mfma32<DT>(f[0], v, acc[i][0]);
-              acc[i][1] = mfma32<DT>(f[1], v, acc[i][1]);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                f32x4& to = DT == 0 && w > 0 ? later[h] : acc[i][h];
+                to = mfma32<DT>(f[h], v, to);
+              }
             }
+            if constexpr (DT == 0 && MT > 1) add_later(i);
           }
         }
+        if constexpr (DT == 0 && MT == 1) add_later(0);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[i][0][e] = fmaf(acc[i][0][e], scale[i], y[i][0][e]);
-            y[i][1][e] = fmaf(acc[i][1][e], scale[i], y[i][1][e]);
+          for (int e = 0; e < 8; ++e) {
+            float v = acc[i][e / 4][e % 4];
+            if constexpr (DT == 0) v *= undo[i];
+            y[i][e / 4][e % 4] = fmaf(v, scale, y[i][e / 4][e % 4]);
           }
         }
       } else if (which >= 0) {
@@ -566,7 +582,7 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
   a.blocks = static_cast<int>((steps + each - 1) / each);
   a.ways = ways_of(MT, a.tiles * a.blocks, a.count, 4 * cus);
   const int rp = (a.rank + 31) / 32 * 32;
-  const size_t lds = static_cast<size_t>(16 * MT) * (2 * kWords<DT> * (rp + 8) + 4);   // (at most 50816 bytes)
+  const size_t lds = static_cast<size_t>(16 * MT) * (2 * kWords * (rp + 8) + 4);   // (at most 50816 bytes)
   const dim3 grid(static_cast<unsigned>(a.tiles * a.ways * a.blocks)), block(kThreads);
   FPSK_LAUNCH(kernel, grid, block, lds, st, a);
   return hipSuccess;

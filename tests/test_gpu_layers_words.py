@@ -78,7 +78,7 @@ def digits(t, rank, fmt, seed):
 
 @pytest.mark.parametrize("t", [20, 1100])
 @pytest.mark.parametrize("rank", [3, 8, 31, 64, 256])
-@pytest.mark.parametrize("fmt", ["bf16"])
+@pytest.mark.parametrize("fmt", ["bf16", "fp16"])
 def test_every_bit_of_the_rank_sums(fl, t, rank, fmt):
     """Column j takes sum j % rank alone."""
     X, A, V = digits(t, rank, fmt, t + rank)
