@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a
   __shared__ __attribute__((aligned(16))) char b0[kShrinkWaves * kBytes];
   __shared__ __attribute__((aligned(16))) char b1[kShrinkWaves * kBytes];
   __shared__ __attribute__((aligned(16))) char b2[kShrinkWaves * kBytes];
-  static_assert(sizeof(float) * kShrinkWaves * TR * (RB + 4) <= sizeof(b0) + sizeof(b1), "");
+  static_assert(sizeof(float) * kShrinkWaves * TR * (RB + 4) <= sizeof(b0), "the waves' sums take the place of b0");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   const ShrinkPart p = shrink_part<TR, RB>(a);
   const int64_t steps = (a.k + kStreamK - 1) / kStreamK, parts = static_cast<int64_t>(kShrinkWaves) * a.splits;

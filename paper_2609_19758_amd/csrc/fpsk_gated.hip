@@ -496,6 +496,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(MmArgs a, int act) {
   const int64_t k0 = wave * run, k1 = k0 + run < a.K ? k0 + run : a.K;
   wave_product<DT, 1, 2>(x, w, r0 + wave * kBytes, r1 + wave * kBytes, r2 + wave * kBytes, k0, k1, acc);
   __syncthreads();
+  static_assert(sizeof(float) * kWaves * kFew * 36 <= sizeof(r0), "the waves' sums take the place of r0");
   auto red = reinterpret_cast<float(*)[kFew][36]>(r0);
 #pragma unroll
   for (int u = 0; u < 2; ++u) *reinterpret_cast<f32x4*>(&red[wave][lane & 15][16 * u + 4 * g]) = acc[0][u];
