@@ -398,10 +398,11 @@ int64_t fpsketch_adapters_workspace(int64_t t, int64_t k, int64_t n, int32_t cou
 /* Heads of a QKV product C (t x (hq + 2 hkv) hd FP32: query, key, value heads of hd entries, hd
  * at most 512): q (t x hq x hd), k and v (t x hkv x hd) in the half format.  Query and key heads
  * are normed with the gains gq, gk (hd FP32 each; both NULL: no norm),
- * x g / sqrt(mean x^2 + eps), then the first rd entries (even, at most hd) are rotated in pairs by
- * pos_i freq_p, p < rd / 2: pairs (p, p + rd / 2), or (2p, 2p + 1) with FPSK_PAIRS_INTERLEAVED.
- * Angles are formed and reduced in FP64; the squares are summed in FP32, so entries of normed heads
- * stay below 2^59.  pos and freq may be NULL when rd is 0. */
+ * x g / sqrt(mean x^2 + eps), with eps 0 or a positive normal number of FP32; then the first rd
+ * entries (even, at most hd) are rotated in pairs by pos_i freq_p, p < rd / 2: pairs (p, p + rd / 2), or
+ * (2p, 2p + 1) with FPSK_PAIRS_INTERLEAVED.  Angles are formed and reduced in FP64; the squares are summed
+ * in FP32, so entries of normed heads stay below 2^59 and, where eps is 0, a head's largest is at least
+ * 2^-58.  pos and freq may be NULL when rd is 0. */
 fpsketch_status fpsketch_heads(const float* C, int64_t t, int32_t hq, int32_t hkv, int32_t hd,
                                const float* gq, const float* gk, double eps, const int64_t* pos,
                                const float* freq, int32_t rd, int32_t pairs, fpsketch_dtype dtype,

@@ -11,6 +11,7 @@
 #include "fpsk_layers.h"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace fpsk {
 
@@ -456,7 +457,11 @@ fpsketch_status heads_check(const char* who, int64_t t, int hq, int hkv, int hd,
   if (rd < 0 || rd > hd || rd % 2 != 0) return bad(FPSK_EINVAL, "rd must be even and at most hd");
   if (pairs != FPSK_PAIRS_HALF && pairs != FPSK_PAIRS_INTERLEAVED) return bad(FPSK_EINVAL, "unknown pairs");
   if ((gq == nullptr) != (gk == nullptr)) return bad(FPSK_EINVAL, "gains for queries or keys only");
-  if (gq != nullptr && !(eps >= 0.0 && std::isfinite(eps))) return bad(FPSK_EINVAL, "eps must be finite and not negative");
+  // eps is held in FP32.  Below its normal numbers it would vanish, and a head of zeros with it become NaN, or
+  // the square of its reciprocal root pass FP32.
+  if (gq != nullptr && !(eps == 0.0 || (eps >= FLT_MIN && eps <= FLT_MAX))) {
+    return bad(FPSK_EINVAL, "eps must be zero or a positive normal number of FP32");
+  }
   if (rd > 0 && t > 0 && (pos == nullptr || freq == nullptr)) return bad(FPSK_EINVAL, "null pos or freq");
   if (!aligned(gq, 4) || !aligned(gk, 4) || !aligned(pos, 8) || !aligned(freq, 4)) {
     return bad(FPSK_EINVAL, "a pointer is not aligned to its elements");

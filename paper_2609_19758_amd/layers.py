@@ -283,7 +283,7 @@ def heads(C, hq: int, hkv: int, pos, freq, fmt: str, gq=None, gk=None, eps: floa
           pairs: str = "half", q=None, k=None, v=None, stream=None):
     """Query, key and value heads of a delivered QKV product C (t x (hq + 2 hkv) hd FP32) in the half
     format ``fmt``: q (t x hq x hd), k and v (t x hkv x hd).  With gains gq, gk (hd FP32) each query
-    and key head is normed, x g / sqrt(mean x^2 + eps); its first 2 len(freq) entries are rotated by
+    and key head is normed, x g / sqrt(mean x^2 + eps) (eps 0 or a normal number of FP32); its first 2 len(freq) entries are rotated by
     pos_i freq_p (pos t int64, freq FP32; freq None: no rotation), in pairs (p, p + len(freq)), or
     (2p, 2p + 1) with ``pairs`` "interleaved"."""
     t, width = _shape(C, "C")
