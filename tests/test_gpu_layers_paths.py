@@ -69,3 +69,60 @@ def test_backward_products_at_any_alignment(fl, t, d, f, shift, fmt):  # noqa: F
     assert beside_x() and beside_w()
     assert torch.equal(fl.gated_products(dP, X, W, need_dw=False)[0], dX)
     assert torch.equal(fl.gated_products(dP, X, W, need_dx=False)[1], dW)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp16"])
+@pytest.mark.parametrize("t,k,n,count,rank", [s[:5] for s in ADAPTERS])
+def test_adapters_of_long_batches(fl, t, k, n, count, rank, fmt):  # noqa: F811
+    """Runs of one adapter and, in between, rows of two or three taking turns."""
+    g, h = rng(t + k + rank), HALF[fmt]
+    X, C = gauss(g, t, k, to=h), gauss(g, t, n)
+    A, B = gauss(g, count, rank, k, std=1 / math.sqrt(k), to=h), gauss(g, count, n, rank, std=0.3, to=h)
+    i = torch.arange(t)
+    first = torch.randint(0, count + 1, (t // 50 + 1,), generator=g)
+    index = ((first[i // 50] + i % (i // 50 % 3 + 1)) % (count + 1) - 1).to(torch.int32)
+    assert sorted(set(index.tolist())) == list(range(-1, count))
+    scale = torch.rand(count, generator=g) * 4 - 2
+    Cg, Xg, Ag, Bg, sg = (placed(v, 1) if k % 8 else v.cuda() for v in (C, X, A, B, scale))
+    (Y, beside) = kept((t, n), 1, torch.float32)
+    fl.adapters(Cg, Xg, Ag, Bg, index.cuda(), sg, out="f32", Y=Y)
+    want, size = C.double(), C.double().abs()
+    for a in range(count):
+        r = (index == a).nonzero().flatten()
+        x, p, q, s = X[r].double(), A[a].double().t(), B[a].double().t(), float(scale[a])
+        want[r] += s * ((x @ p) @ q)
+        size[r] += abs(s) * ((x.abs() @ p.abs()) @ q.abs())
+    within(Y, want, size * (k + rank + 8) * 2 * U, "Y")
+    assert beside() and torch.equal(Y.cpu()[index == -1], C[index == -1])
+    assert torch.equal(fl.adapters(Cg, Xg, Ag, Bg, index.cuda(), sg), Y.to(h))
+
+
+@pytest.mark.parametrize("fmt,pairs", [("bf16", "half"), ("fp16", "interleaved")])
+@pytest.mark.parametrize("t,hq,hkv,hd,rd", [s[:5] for s in GAINS])
+def test_gains_of_long_batches(fl, t, hq, hkv, hd, rd, fmt, pairs):  # noqa: F811
+    g, h, eps = rng(t + hd), HALF[fmt], 1e-5
+    C = gauss(g, t, (hq + 2 * hkv) * hd, std=1.5)
+    gains = [gauss(g, hd, std=0.5) + 1, gauss(g, hd, std=0.5) - 1]
+    pos = torch.randint(0, 1 << 20, (t,), generator=g)
+    freq = torch.pow(10000.0, -torch.arange(rd // 2, dtype=torch.float64) * 2 / rd).float()
+    # (a mean of their own, so that the sums grow with the tokens)
+    d = [gauss(g, t, n, hd, std=0.5, to=h) + 0.25 for n in (hq, hkv, hkv)]
+    kw = dict(eps=eps, pairs=pairs)
+    dC, dgq, dgk = fl.heads_grad(*[x.cuda() for x in d], C.cuda(), pos.cuda(), freq.cuda(), gq=gains[0].cuda(),
+                                 gk=gains[1].cuda(), **kw)
+    leaves = [C.double().requires_grad_(True)] + [x.double().requires_grad_(True) for x in gains]
+    out = heads64(leaves[0], hq, hkv, hd, pos, freq, leaves[1], leaves[2], eps, pairs)
+    grads = torch.autograd.grad(out, leaves, [x.double() for x in d])
+    x = C.double().view(t, -1, hd)
+    xr = (x * torch.rsqrt((x * x).mean(-1, keepdim=True) + eps)).abs()
+    for got, want, part, dy in ((dgq, grads[1], xr[:, :hq], d[0]), (dgk, grads[2], xr[:, hq:hq + hkv], d[1])):
+        # an entry rotated back: at most sqrt(2) of the head's largest
+        size = (part * dy.double().abs().amax(-1, keepdim=True) * 1.5).sum((0, 1))
+        # every work-group's sum is of its own tokens and heads, 1/1024 of them, in FP32; their sum in FP64
+        terms = -(-t // 1024) * part.shape[1] + 8
+        within(got, want, size * (2 * terms + hd + 40) * U, "gain")
+    # the last tokens, which a work-group takes after others, are those of a call on them alone
+    tail = 100
+    alone = fl.heads_grad(*[v[-tail:].contiguous().cuda() for v in d], C[-tail:].contiguous().cuda(),
+                          pos[-tail:].contiguous().cuda(), freq.cuda(), gq=gains[0].cuda(), gk=gains[1].cuda(), **kw)
+    assert torch.equal(alone[0], dC[-tail:])
