@@ -126,3 +126,38 @@ def test_gains_of_long_batches(fl, t, hq, hkv, hd, rd, fmt, pairs):  # noqa: F81
     alone = fl.heads_grad(*[v[-tail:].contiguous().cuda() for v in d], C[-tail:].contiguous().cuda(),
                           pos[-tail:].contiguous().cuda(), freq.cuda(), gq=gains[0].cuda(), gk=gains[1].cuda(), **kw)
     assert torch.equal(alone[0], dC[-tail:])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_faulty_products_reach_the_gradient(fl, act):  # noqa: F811
+    """Infinite and NaN entries of P show in the entries of dP that they enter, and in no other."""
+    f, inf, nan = 4, float("inf"), float("nan")
+    P = torch.ones(4, 2 * f)
+    P[0, 1], P[1, f + 2], P[2, 3], P[3, f] = inf, nan, nan, -inf
+    dH = torch.full((4, f), 2.0, dtype=torch.bfloat16).cuda()
+    dP, dPt = fl.gated_grad(dH, P.cuda(), act=act, transpose=True)
+    assert torch.equal(dPt.t().isnan(), dP.isnan()) and torch.equal(dPt.t().isinf(), dP.isinf())
+    dP = dP.cpu()
+    assert dP[0, f + 1] == inf                              # dU = dH act(inf)
+    assert torch.isnan(dP[1, 2]) and torch.isnan(dP[2, 3]) and torch.isnan(dP[2, f + 3])
+    assert dP[3, 0] == -inf                                 # dG = dH U act'(1), act'(1) > 0
+    assert int((~torch.isfinite(dP)).sum()) == 5
+    H = fl.gated_narrow(P.cuda(), "bf16", act=act).cpu()
+    assert H[0, 1] == inf and torch.isnan(H[1, 2]) and torch.isnan(H[2, 3]) and H[3, 0] == -inf
+    assert int((~torch.isfinite(H)).sum()) == 4
+
+
+def test_the_smallest_eps(fl):  # noqa: F811
+    """A head of zeros is zero with the smallest eps there is, and so is its gradient where the output's is."""
+    hd, t = 64, 3
+    C, gain = torch.zeros(t, 4 * hd).cuda(), torch.ones(hd).cuda()
+    pos, freq = torch.arange(t).cuda(), torch.ones(hd // 2).cuda()
+    kw = dict(gq=gain, gk=gain, eps=2.0 ** -126)
+    q, k, v = fl.heads(C, 2, 1, pos, freq, "bf16", **kw)
+    assert not q.any() and not k.any() and not v.any()
+    for n in (hd, 33):                                       # both kernels
+        z = [torch.zeros(t, m, n, dtype=torch.bfloat16).cuda() for m in (2, 1, 1)]
+        g = torch.ones(n).cuda()
+        dC, dgq, dgk = fl.heads_grad(*z, torch.zeros(t, 4 * n).cuda(), pos, freq[:8].contiguous(), gq=g, gk=g,
+                                     eps=2.0 ** -126)
+        assert not dC.any() and not dgq.any() and not dgk.any()
