@@ -510,21 +510,12 @@ __global__ __launch_bounds__(kThreads) void tiny_kernel(AdapterArgs a, int half)
 // short ones (48 tokens 15.7 us, 16.6 in tiles of 32); k in up to 8 parts while the tiles do not give
 // every compute unit two work-groups (4093 tokens without parts 81.5 us); and as many work-groups to a
 // tile's adapters as that leaves room for.
-struct Cut {
-  int mt, ways;
-  int64_t tiles;
-};
-
 struct Plan {
-  Cut shrink, expand;
-  int splits, nt, rank_blocks, ldv;
+  int mt;                  // 16-row blocks of a tile
+  int64_t tiles;
+  int splits, ways, nt, rank_blocks, ldv;   // of the first product (the second's: launch_expand)
   bool direct;
 };
-
-Cut tiles_of(int64_t t, int mt) {
-  const int tr = 16 * mt;
-  return {mt, 1, (t + tr - 1) / tr};
-}
 
 // Work-groups to a tile's adapters, where there are `groups` with one each.
 int ways_of(int mt, int64_t groups, int count, int cus) {
@@ -538,12 +529,12 @@ Plan plan_of(int64_t t, int64_t k, int count, int rank, bool direct, int cus) {
   p.nt = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
   p.rank_blocks = (rank + 16 * p.nt - 1) / (16 * p.nt);
   p.ldv = (rank + 3) / 4 * 4;
-  p.shrink = tiles_of(t, t > 1024 ? 2 : 1);
-  p.expand = tiles_of(t, t > 1024 ? 2 : 1);
-  const int64_t steps = (k + 63) / 64, groups = p.shrink.tiles * p.rank_blocks;
+  p.mt = t > 1024 ? 2 : 1;
+  p.tiles = (t + 16 * p.mt - 1) / (16 * p.mt);
+  const int64_t steps = (k + 63) / 64, groups = p.tiles * p.rank_blocks;
   p.splits = static_cast<int>(
       std::max<int64_t>(1, std::min<int64_t>({2 * cus / groups, steps / kShrinkWaves, int64_t{kMaxSplits}})));
-  p.shrink.ways = ways_of(p.shrink.mt, groups * p.splits, count, cus);
+  p.ways = ways_of(p.mt, groups * p.splits, count, cus);
   return p;
 }
 
@@ -562,8 +553,7 @@ hipError_t launch_shrink(const AdapterArgs& a, bool direct, hipStream_t st) {
 
 template <int DT, int MT>
 hipError_t launch_shrink(AdapterArgs a, const Plan& p, hipStream_t st) {
-  a.tiles = p.shrink.tiles;
-  a.ways = p.shrink.ways;
+  a.ways = p.ways;
   a.blocks = p.rank_blocks;
   if (p.nt == 1) return launch_shrink<DT, MT, 1>(a, p.direct, st);
   if (p.nt == 2) return launch_shrink<DT, MT, 2>(a, p.direct, st);
@@ -590,9 +580,9 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
 
 template <int DT, int MT>
 hipError_t launch_adapters(AdapterArgs a, const Plan& p, bool half, int cus, hipStream_t st) {
-  const hipError_t e = p.shrink.mt == 2 ? launch_shrink<DT, 2>(a, p, st) : launch_shrink<DT, 1>(a, p, st);
+  a.tiles = p.tiles;
+  const hipError_t e = launch_shrink<DT, MT>(a, p, st);
   if (e != hipSuccess) return e;
-  a.tiles = p.expand.tiles;
   if (a.rank % 8 == 0) return half ? launch_expand<DT, MT, true, true>(a, cus, st) : launch_expand<DT, MT, false, true>(a, cus, st);
   return half ? launch_expand<DT, MT, true, false>(a, cus, st) : launch_expand<DT, MT, false, false>(a, cus, st);
 }
@@ -642,8 +632,8 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
   const Plan p = plan_of(t, k, count, rank, k % 8 == 0 && k <= kMaxLd && aligned(X, 16) && aligned(A, 16), cus);
   const int64_t need = space_of(p, t);
   // work-groups of the two launches
-  if (static_cast<double>(p.shrink.tiles) * p.shrink.ways * p.rank_blocks * p.splits * kThreads >= 4294967296.0 ||
-      (static_cast<double>(p.expand.tiles) * ((n + 127) / 128) + 64.0 * cus) * kThreads >= 4294967296.0) {
+  if (static_cast<double>(p.tiles) * p.ways * p.rank_blocks * p.splits * kThreads >= 4294967296.0 ||
+      (static_cast<double>(p.tiles) * ((n + 127) / 128) + 64.0 * cus) * kThreads >= 4294967296.0) {
     return layer_error(FPSK_ESHAPE, "fpsketch_adapters: too many tiles");
   }
   if (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 16)) {
@@ -676,9 +666,9 @@ fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, 
     e = dtype == FPSK_BF16 ? launch_k(tiny_kernel<1>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half})
                            : launch_k(tiny_kernel<0>, grid, dim3(kThreads), 0, st, nullptr, nullptr, a, int{half});
   } else if (dtype == FPSK_BF16) {
-    e = p.expand.mt == 2 ? launch_adapters<1, 2>(a, p, half, cus, st) : launch_adapters<1, 1>(a, p, half, cus, st);
+    e = p.mt == 2 ? launch_adapters<1, 2>(a, p, half, cus, st) : launch_adapters<1, 1>(a, p, half, cus, st);
   } else {
-    e = p.expand.mt == 2 ? launch_adapters<0, 2>(a, p, half, cus, st) : launch_adapters<0, 1>(a, p, half, cus, st);
+    e = p.mt == 2 ? launch_adapters<0, 2>(a, p, half, cus, st) : launch_adapters<0, 1>(a, p, half, cus, st);
   }
   return launched(e, "fpsketch_adapters");
 }
