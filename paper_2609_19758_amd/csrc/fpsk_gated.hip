@@ -1018,11 +1018,12 @@ ProductsPlan plan_products(const void* dP, const void* X, const void* W, int64_t
   if (!take_w) g.p = p;
   if (take_x) copy_padded(g.w, space, g.pad, g.pads);
   if (take_w) copy_padded(g.x, space, g.pad, g.pads);
-  if (!g.dx.big && !g.dw.big) {
+  const bool share = direct_x && direct_w && !g.dx.big && !g.dw.big;   // a launch, where both are asked for
+  if (share) {
     fewer_parts(g.dx, 2 * f, 2 * cus - g.dw.tiles_m * g.dw.tiles_n);
     fewer_parts(g.dw, t, 2 * cus - g.dx.tiles_m * g.dx.tiles_n);
   }
-  g.pair = take_x && take_w && !g.dx.big && !g.dw.big;
+  g.pair = take_x && take_w && share;
   const int64_t px = need_dx && t > 0 ? part_bytes(g.dx, t, d) : 0, pw = need_dw ? part_bytes(g.dw, 2 * f, d) : 0;
   if (g.pair) {
     g.part_x = static_cast<float*>(space.take(px));

@@ -32,9 +32,10 @@ GAINS = [(2500, 4, 2, 128, 64, {"heads_grad_vec", "gains"}), (2500, 3, 1, 33, 20
          (2500, 2, 2, 80, 20, {"heads_grad", "gains"}), (2300, 1, 1, 512, 512, {"heads_grad_vec", "gains"})]
 
 
-def test_routes(runtime):  # noqa: F811
+@pytest.mark.parametrize("scenario", ["routes", "apart"])
+def test_launches(runtime, scenario):  # noqa: F811
     env = dict(os.environ, PYTHONPATH=ROOT)
-    res = subprocess.run([sys.executable, os.path.abspath(__file__), runtime],
+    res = subprocess.run([sys.executable, os.path.abspath(__file__), runtime, scenario],
                          capture_output=True, text=True, timeout=100, env=env)
     assert res.returncode == 0, res.stdout + res.stderr
 
@@ -42,25 +43,37 @@ def test_routes(runtime):  # noqa: F811
 # ---- in the process of its own -------------------------------------------------------------
 
 
-def routes(h):
-    def launched(call):
-        h.rt.rt_reset()
-        assert call() == fk.OK, (call.name, h.error())
-        return [(re.sub(r".*12_GLOBAL__N_1\d+(\w+?)_kernel.*", r"\1", k), g) for k, g in h.kernels()]
+def launched(h, call):
+    h.rt.rt_reset()
+    assert call() == fk.OK, (call.name, h.error())
+    return [(re.sub(r".*12_GLOBAL__N_1\d+(\w+?)_kernel.*", r"\1", k), g) for k, g in h.kernels()]
 
+
+def routes(h):
     for C, shapes in ((Gated, GATED), (Products, PRODUCTS)):
         for t, d, f, shift, want in shapes:
-            got = {k for k, _ in launched(C(h, t=t, d=d, f=f, shift=2 * shift))}
+            got = {k for k, _ in launched(h, C(h, t=t, d=d, f=f, shift=2 * shift))}
             assert got - {"pad", "mm_sum"} == want, (C.name, t, d, f, shift, got)
     for t, k, n, count, rank, want in ADAPTERS:
-        got = dict(launched(Adapters(h, t=t, d=k, f=n, count=count, rank=rank)))
+        got = dict(launched(h, Adapters(h, t=t, d=k, f=n, count=count, rank=rank)))
         assert set(got) == want, (t, k, n, got)
     # the last one: a work-group takes several blocks of 128 columns
     assert got["expand"] < -(-t // 32) * -(-n // 128), got
     for t, hq, hkv, hd, rd, want in GAINS:
-        got = launched(HeadsGrad(h, t=t, hq=hq, hkv=hkv, hd=hd, rd=rd))
+        got = launched(h, HeadsGrad(h, t=t, hq=hq, hkv=hkv, hd=hd, rd=rd))
         assert {k for k, _ in got} == want and got[0][1] < t, (t, hd, got)
 
 
+def apart(h):
+    """A product that does not share its launch is cut for the whole chip: dX in as many parts as it takes to
+    give 256 compute units a work-group each (at most 32, of at least 4 steps of 64 k), whatever dW's size."""
+    for t, d, f in [(7, 1, 700001), (50, 1555, 4608), (200, 4101, 600), (972, 64, 2546)]:
+        got = [(k, g) for k, g in launched(h, Products(h, t=t, d=d, f=f)) if k in ("mm", "mm_ragged")]
+        tiles, steps = -(-t // 128) * -(-d // 128), -(-2 * f // 64)
+        if got[0][0] == "mm_ragged":
+            most = min(32, steps // 4)
+            assert got[0][1] >= min(256, tiles * most) * 3 // 4, (t, d, f, got, tiles, steps)
+
+
 if __name__ == "__main__":
-    routes(Host(sys.argv[1]))
+    globals()[sys.argv[2]](Host(sys.argv[1]))
