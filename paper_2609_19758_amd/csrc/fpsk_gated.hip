@@ -763,16 +763,20 @@ struct Cut {
 
 // Microseconds that a product of M x N takes in `tiles` tiles and `splits` parts of `per` steps, by
 // what the kernels measure: a step of 64 k takes 1.66 us in a tile of 256, 1.1 us in two of 128 side by
-// side and 0.6 us in one alone; a round of work-groups begins and ends in 5 and 3 us; operands come
-// from memory at 4.3 TB/s, 3.4 with a single tile of 128 per compute unit; and parts are written, read
-// and added at 5 TB/s in a launch of 3 us.  (4096 x 22016 x 4096: 667 us, measured 672; 500 x 22016 x
-// 4096: 111 and 110, where 256-tiles in two parts take 145 and 128-tiles 144; 1000 x 8192 x 4096: 73
-// and 67, in 256-tiles 79 in two parts, 93 in one; 67 x 27648 x 5120: 75 and 72, 86 in one part.)
-double cost(bool big, double M, double N, double K, int64_t tiles, int64_t splits, int64_t per, int cus) {
+// side and 0.6 us in one alone (2.8 and 2.35 us through registers, where it waits for its own loads); a
+// round of work-groups begins and ends in 5 and 3 us; operands come from memory at 4.3 TB/s, 3.4 with a
+// single tile of 128 per compute unit; and parts are written, read and added at 5 TB/s in a launch of 3 us.
+// (4096 x 22016 x 4096: 667 us, measured 672; 500 x 22016 x 4096: 111 and 110, where 256-tiles in two parts
+// take 145 and 128-tiles 144; 1000 x 8192 x 4096: 73 and 67, in 256-tiles 79 in two parts, 93 in one; 67 x
+// 27648 x 5120: 75 and 72, 86 in one part; 130 x 8192 x 4095 through registers: 55 and 56, 85 in
+// two parts.)
+double cost(bool big, bool direct, double M, double N, double K, int64_t tiles, int64_t splits, int64_t per,
+            int cus) {
   const int64_t groups = tiles * splits, slots = big ? cus : 2 * cus, rest = groups % slots;
-  const double steps = static_cast<double>(per), round = big ? 1.66 * steps + 5 : 1.1 * steps + 3;
+  const double steps = static_cast<double>(per);
+  const double round = big ? 1.66 * steps + 5 : (direct ? 1.1 : 2.8) * steps + 3;
   double c = static_cast<double>(groups / slots) * round;
-  if (rest > 0) c += big || rest > cus ? round : 0.6 * steps + 3;
+  if (rest > 0) c += big || rest > cus ? round : (direct ? 0.6 : 2.35) * steps + 3;
   c = std::max(c, 2e-6 * K * (M + N) / (big || groups > cus ? 4.3 : 3.4));
   return splits == 1 ? c : c + 3 + 8e-6 / 5 * static_cast<double>(splits) * M * N;
 }
@@ -798,7 +802,7 @@ Cut cut_of(int64_t M, int64_t cols, bool gated, bool few, int64_t K, bool direct
     const int64_t most = std::min<int64_t>({32, std::max<int64_t>(1, steps / 4), 1 + 2 * cus / (tm * tn)});
     for (int64_t s = 1; s <= most; ++s) {
       const int64_t per = (steps + s - 1) / s, parts = (steps + per - 1) / per;
-      const double t = cost(big, static_cast<double>(M), static_cast<double>(gated ? 2 * cols : cols),
+      const double t = cost(big, direct, static_cast<double>(M), static_cast<double>(gated ? 2 * cols : cols),
                             static_cast<double>(K), tm * tn, parts, per, cus);
       if (best >= 0.0 && t >= best) continue;
       best = t;
@@ -826,9 +830,9 @@ void fewer_parts(Cut& c, int64_t K, int64_t room) {
 bool fits(const void* p, int64_t ld) { return ld % 8 == 0 && aligned(p, 16); }
 
 // Whether a product is worth padded copies of the `elements` that do not fit: small ones, whose copy is
-// one short launch (gated 400 x 1023 x 1000: 21 us, 29 us with the kernel for any alignment), and
-// those with the work to make up for it (4095 x 4096: 63 against 91 us at 300 tokens, but 58 against
-// 52 us at 130 and 42 against 29 us at 20).
+// one short launch (gated 400 x 1023 x 1000: 23 us either way), and those with the work to make up for it
+// (4095 x 4096: 71 against 98 us through registers at 300 tokens, but 56 and 59 us at 200, 55 and 56 at 130 and
+// 43 against 31 us at 20).
 bool worth_copies(int64_t elements, int64_t M, int64_t N, int64_t K) {
   return elements <= int64_t{1} << 22 || 256.0 * static_cast<double>(elements) <= static_cast<double>(M) * N * K;
 }

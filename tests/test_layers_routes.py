@@ -32,7 +32,7 @@ GAINS = [(2500, 4, 2, 128, 64, {"heads_grad_vec", "gains"}), (2500, 3, 1, 33, 20
          (2500, 2, 2, 80, 20, {"heads_grad", "gains"}), (2300, 1, 1, 512, 512, {"heads_grad_vec", "gains"})]
 
 
-@pytest.mark.parametrize("scenario", ["routes", "apart"])
+@pytest.mark.parametrize("scenario", ["routes", "apart", "registers"])
 def test_launches(runtime, scenario):  # noqa: F811
     env = dict(os.environ, PYTHONPATH=ROOT)
     res = subprocess.run([sys.executable, os.path.abspath(__file__), runtime, scenario],
@@ -73,6 +73,14 @@ def apart(h):
         if got[0][0] == "mm_ragged":
             most = min(32, steps // 4)
             assert got[0][1] >= min(256, tiles * most) * 3 // 4, (t, d, f, got, tiles, steps)
+
+
+def registers(h):
+    """A product through registers, whose steps are mostly waiting, gives every compute unit two work-groups where
+    K has the steps for it."""
+    for t in (20, 50, 100, 130):
+        got = launched(h, Gated(h, t=t, d=4095, f=4096))
+        assert got[0][0] == "mm_ragged" and 448 <= got[0][1] <= 512, (t, got)
 
 
 if __name__ == "__main__":
