@@ -345,17 +345,22 @@ double fpsketch_rms_hat_samples(const float* samples, int64_t count);
 /* may be 0 and then NULL), aligned to 16 bytes; it belongs to the call until its work on      */
 /* `stream` is done, so calls that may overlap in time (other streams, graphs replayed beside  */
 /* each other) each need their own.  Sums, products and statistics are held in FP32 or more,   */
-/* and each result is rounded once.  FPSK_ESHAPE: a dimension outside [1, 2^31) (t: [0, 2^31); */
-/* gated block: d and 2f at most 2^22) or an array of more than 2^40 elements; FPSK_EINVAL:    */
-/* null or misaligned pointers and the rest.                                                   */
+/* and each result is rounded once.  Activations take the hardware's exponential and           */
+/* reciprocal, a few units of FP32's last place; below a gate of about -88 silu and the tanh   */
+/* form are 0.  FPSK_ESHAPE: a dimension outside [1, 2^31) (t: [0, 2^31); gated block: d and   */
+/* 2f at most 2^22; heads: hd at most 512, hq and hkv at most 65536; adapters: rank at most    */
+/* 256), an array of more than 2^40 elements, or a launch of more work-groups than the runtime */
+/* takes (2^32 threads); FPSK_EINVAL: null or misaligned pointers and the rest.                */
 
 typedef enum { FPSK_SILU = 0, FPSK_GELU = 1, FPSK_GELU_TANH = 2 } fpsketch_act;
 typedef enum { FPSK_PAIRS_HALF = 0, FPSK_PAIRS_INTERLEAVED = 1 } fpsketch_pairs;
 
 /* Gated feed-forward: P = X W^T with X t x d and the stacked weight W 2f x d (f gate rows, then f
- * up rows), and H = act(G) U (t x f, half format) with G = P[:, :f], U = P[:, f:], in one kernel.
- * H is formed from the FP32 products.  P (t x 2f FP32) is delivered when not NULL: it is the C of
- * a context (t, d, 2f, dtype) with b_layout 1 and B = W. */
+ * up rows), and H = act(G) U (t x f, half format) with G = P[:, :f], U = P[:, f:].  H is formed from
+ * the FP32 products where they are summed, so P is not read again: one kernel, with one before it
+ * where operands off 16-byte groups are copied and one after it where d is cut into parts.  P (t x 2f
+ * FP32) is delivered when not NULL: it is the C of a context (t, d, 2f, dtype) with b_layout 1 and
+ * B = W. */
 fpsketch_status fpsketch_gated(const void* X, const void* W, int64_t t, int64_t d, int64_t f,
                                fpsketch_dtype dtype, fpsketch_act act, void* H, float* P,
                                void* workspace, int64_t workspace_bytes, void* stream);
@@ -386,7 +391,9 @@ int64_t fpsketch_gated_products_workspace(const void* dP, const void* X, const v
  * Y_i = C_i + scale_a (X_i A_a^T) B_a^T with a = index_i, X t x k, A count x rank x k and
  * B count x n x rank (rank 1 to 256; adapters of a smaller rank are padded with zeros).  index -1:
  * no adapter, Y_i = C_i; any other index outside [0, count) makes the row NaN.  Y (t x n) is in
- * the half format, or in FP32 with y_dtype FPSK_F32.  Rows of one adapter need not be neighbours.
+ * the half format, or in FP32 with y_dtype FPSK_F32.  Rows of one adapter need not be neighbours,
+ * but runs of them are faster.  The rank sums X_i A_a^T keep FP32's 24 bits; an infinite entry of B
+ * makes what it enters NaN.
  * C is not modified, so that it can still be localized and repaired. */
 fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, const void* B,
                                   const int32_t* index, const float* scale, int64_t t, int64_t k,
@@ -399,10 +406,11 @@ int64_t fpsketch_adapters_workspace(int64_t t, int64_t k, int64_t n, int32_t cou
  * at most 512): q (t x hq x hd), k and v (t x hkv x hd) in the half format.  Query and key heads
  * are normed with the gains gq, gk (hd FP32 each; both NULL: no norm),
  * x g / sqrt(mean x^2 + eps), with eps 0 or a positive normal number of FP32; then the first rd
- * entries (even, at most hd) are rotated in pairs by pos_i freq_p, p < rd / 2: pairs (p, p + rd / 2), or
- * (2p, 2p + 1) with FPSK_PAIRS_INTERLEAVED.  Angles are formed and reduced in FP64; the squares are summed
- * in FP32, so entries of normed heads stay below 2^59 and, where eps is 0, a head's largest is at least
- * 2^-58.  pos and freq may be NULL when rd is 0. */
+ * entries (even, at most hd) are rotated in pairs by pos_i freq_p, p < rd / 2: pairs (p, p + rd / 2),
+ * or (2p, 2p + 1) with FPSK_PAIRS_INTERLEAVED.  Angles are formed and reduced in FP64, then rounded to
+ * FP32 (at most half a turn: 2^-23); the squares are summed in FP32, so entries of normed heads stay
+ * below 2^59 and, where eps is 0, a head's largest is at least 2^-58.  pos and freq may be NULL when rd
+ * is 0. */
 fpsketch_status fpsketch_heads(const float* C, int64_t t, int32_t hq, int32_t hkv, int32_t hd,
                                const float* gq, const float* gk, double eps, const int64_t* pos,
                                const float* freq, int32_t rd, int32_t pairs, fpsketch_dtype dtype,

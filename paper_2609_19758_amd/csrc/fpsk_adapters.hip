@@ -36,7 +36,8 @@ struct AdapterArgs {
 // rows name: an adapter's factor multiplies the whole tile on the matrix cores, and only its own rows
 // are kept.  The rows of a request are neighbours, so a prompt's tile names one adapter or two and no
 // sorting of rows is needed before; a decode tile names up to 16, which `ways` work-groups take in turn
-// (48 tokens of 24 adapters: 15.7 us, 40.6 with one work-group to a tile).
+// (48 tokens of 24 adapters: 14.9 us, 41.0 with one work-group to a tile).  What a tile costs grows with the
+// adapters it names: 256 tokens of 64 adapters take 36 us one by one and 15 us in 16 runs.
 //
 // each(a, mask): a the adapter (-1: none, count: invalid), mask its rows in the tile.
 template <int TR, typename F>
@@ -95,9 +96,9 @@ __device__ __forceinline__ void shrink_store(const AdapterArgs& a, const ShrinkP
 
 // V = X A^T, both streamed through LDS; the parts of k are added by the next kernel, in order.  Bound
 // by reading X and by how few bytes of it the factor's rows leave room for under way: 4093 x 11008 at
-// rank 64 takes 39 us (2.3 TB/s of X), 31.8 us where every tile names one adapter; more parts of k or
-// two work-groups to every tile take longer (76.7 us for both kernels, 82 and 77).  48 x 4096 at rank
-// 16, 24 adapters: 6.1 us.
+// rank 64 takes 39 us (2.3 TB/s of X; 106 MB come from memory for 90 of X), 31.8 us where every tile names one
+// adapter; more parts of k or two work-groups to every tile take longer (75.5 us for both kernels, 83.6 and
+// 79.3).  48 x 4096 at rank 16, 24 adapters: 6.0 us.
 template <int DT, int MT, int NT>
 __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(AdapterArgs a) {
   constexpr int TR = 16 * MT, RB = 16 * NT, kBytes = WaveRows<MT>::kBytes + WaveRows<NT>::kBytes;
@@ -506,9 +507,9 @@ __global__ __launch_bounds__(kThreads) void tiny_kernel(AdapterArgs a, int half)
 // ---- host ------------------------------------------------------------------------------------
 
 // How the work is cut: tiles of 32 rows in long batches (each factor is then read from L2 half as
-// often: 4093 tokens at rank 64 take 77 us, 103 in tiles of 16; 1500 at rank 16 22.4 and 23.9), of 16 in
-// short ones (48 tokens 15.7 us, 16.6 in tiles of 32); k in up to 8 parts while the tiles do not give
-// every compute unit two work-groups (4093 tokens without parts 81.5 us); and as many work-groups to a
+// often: 4093 tokens at rank 64 take 76 us, 92 in tiles of 16; 1500 at rank 16 24.4 and 26.6), of 16 in
+// short ones (48 tokens 15.2 us, 18.3 in tiles of 32); k in up to 8 parts while the tiles do not give
+// every compute unit two work-groups (4093 tokens without parts 80 us); and as many work-groups to a
 // tile's adapters as that leaves room for.
 struct Plan {
   int mt;                  // 16-row blocks of a tile
@@ -565,8 +566,8 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
   const auto kernel = expand_kernel<DT, MT, HALF, WHOLE>;
   // A work-group forms the tile's V once for all its columns: so many of them that three work-groups
   // are left for every compute unit, but no more than the rank is worth, since later work-groups even
-  // out what is left at the end (8192 x 11008: rank 128 267 us without that bound, 211 us; rank 16 178
-  // and 146 us; with one block each rank 256 at 4096 x 4096 takes 139 us, not 118).
+  // out what is left at the end (8192 x 11008: rank 128 261 us without that bound, 200 us; rank 16 160
+  // and 140 us; with one block each rank 256 at 4096 x 4096 takes 96 us, not 83).
   const int64_t steps = (a.n + kColumns - 1) / kColumns;
   const int64_t each = std::max<int64_t>(1, std::min<int64_t>({steps, a.tiles * steps / (3 * cus), a.rank / 32}));
   a.blocks = static_cast<int>((steps + each - 1) / each);

@@ -14,6 +14,8 @@ As in ``fpsketch``, this is argument marshalling only: every step runs in the li
 Operands are torch tensors, contiguous and on one GPU; they are checked before the library is
 called.  The work is enqueued on ``stream`` (default: torch's current stream of the operands' GPU),
 and outputs and workspaces are allocated on that stream, so a call can be captured into a graph.
+None of it is recorded by autograd: operands that require gradients are taken as they are and results
+carry none; the ``_grad`` and ``_products`` calls are the backward passes, called by name.
 """
 from __future__ import annotations
 
@@ -121,7 +123,7 @@ class _Call:
 
 
 def gated(X, W, act: str = "silu", deliver: bool = True, H=None, P=None, stream=None):
-    """H = act(G) U with [G U] = P = X W^T, in one kernel.  X (t x d) and W (2f x d: f gate rows, then
+    """H = act(G) U with [G U] = P = X W^T, without another pass over P.  X (t x d) and W (2f x d: f gate rows, then
     f up rows) in one half format; returns H (t x f, that format) and P (t x 2f FP32, the C of a
     ``Verifier(t, d, 2 * f, fmt, b_layout=1)`` with B = W), or None in its place with ``deliver``
     false.  ``H`` and ``P``: buffers to write into."""
@@ -283,9 +285,9 @@ def heads(C, hq: int, hkv: int, pos, freq, fmt: str, gq=None, gk=None, eps: floa
           pairs: str = "half", q=None, k=None, v=None, stream=None):
     """Query, key and value heads of a delivered QKV product C (t x (hq + 2 hkv) hd FP32) in the half
     format ``fmt``: q (t x hq x hd), k and v (t x hkv x hd).  With gains gq, gk (hd FP32) each query
-    and key head is normed, x g / sqrt(mean x^2 + eps) (eps 0 or a normal number of FP32); its first 2 len(freq) entries are rotated by
-    pos_i freq_p (pos t int64, freq FP32; freq None: no rotation), in pairs (p, p + len(freq)), or
-    (2p, 2p + 1) with ``pairs`` "interleaved"."""
+    and key head is normed, x g / sqrt(mean x^2 + eps) (eps 0 or a normal number of FP32); its first
+    2 len(freq) entries are rotated by pos_i freq_p (pos t int64, freq FP32; freq None: no rotation), in
+    pairs (p, p + len(freq)), or (2p, 2p + 1) with ``pairs`` "interleaved"."""
     t, width = _shape(C, "C")
     dt, h = _code(_FMT, fmt, "fmt")
     if hq < 1 or hkv < 1 or width % (hq + 2 * hkv):
