@@ -392,8 +392,7 @@ int64_t fpsketch_gated_products_workspace(const void* dP, const void* X, const v
  * B count x n x rank (rank 1 to 256; adapters of a smaller rank are padded with zeros).  index -1:
  * no adapter, Y_i = C_i; any other index outside [0, count) makes the row NaN.  Y (t x n) is in
  * the half format, or in FP32 with y_dtype FPSK_F32.  Rows of one adapter need not be neighbours,
- * but runs of them are faster.  The rank sums X_i A_a^T keep FP32's 24 bits; an infinite entry of B
- * makes what it enters NaN.
+ * but runs of them are faster.  The rank sums X_i A_a^T keep FP32's 24 bits.
  * C is not modified, so that it can still be localized and repaired. */
 fpsketch_status fpsketch_adapters(const float* C, const void* X, const void* A, const void* B,
                                   const int32_t* index, const float* scale, int64_t t, int64_t k,

@@ -248,7 +248,8 @@ constexpr int kColumns = 128;   // of a work-group at a time, 32 per wave
 // each, the later two 2^12 times as large, so that they are in FP16's range wherever the first is (sums are
 // scaled to below 2^15 before).
 constexpr int kWords = 3;
-constexpr float kLater = 4096.0f;
+template <int DT>
+constexpr float kLater = DT == 0 ? 4096.0f : 1.0f;
 
 template <int DT>
 __device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords]) {
@@ -257,7 +258,7 @@ __device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords]) {
   // (BF16: a finite sum that would round to infinity keeps the largest number as its first word)
   if (DT == 1 && (w[0] & 0x7fffu) == 0x7f80u && finite) w[0] -= 1;
   float rest = s - from_half<DT>(w[0]);    // (exact, as is each one after it)
-  if constexpr (DT == 0) rest *= kLater;
+  rest *= kLater<DT>;
 #pragma unroll
   for (int i = 1; i < kWords; ++i) {
     w[i] = finite ? to_half<DT>(rest) : uint16_t{0};
@@ -270,7 +271,7 @@ __device__ __forceinline__ void split_words(float s, uint16_t (&w)[kWords]) {
 // products so that a lane holds 8 neighbours of one row.  V enters the matrix cores as half words
 // (split_words) against the exact factor B; in FP16 a row is first scaled by a power of two that puts its
 // largest sum at 2^14, and its later words have sums of their own.  4093 x 4096 at rank 64 in FP16: 36.4 us,
-// 2.8 TB/s (36.3 with two words, which lose bits; 8192 x 11008 at rank 128 205 and 198, 4096 x 4096 at rank 256 87
+// 2.8 TB/s (36.3 with two words, which lose bits; 8192 x 11008 at rank 128 207 and 198, 4096 x 4096 at rank 256 90
 // and 79); 48 x 4096 at rank 16, 24 adapters, in BF16: 8.9 us (8.7).
 //
 // WHOLE: the rank is a multiple of 8, so that a group of 8 ranks lies in a row of B or outside.
@@ -389,13 +390,16 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
         }
       }
       if (mine) {
-        // FP16's later words: summed over all ranks in one row of blocks, per 32 ranks in two (over all of them
-        // 4093 x 4096 takes 72 registers and 40 us, not 64 and 36; 48 tokens take 8.9 us, per 32 ranks 10.4)
+        // The later words: summed over all ranks in one row of blocks, per 32 ranks in two (over all of them
+        // 4093 x 4096 in FP16 takes 72 registers and 40 us, not 64 and 36; 48 tokens take 8.9 us, per 32 ranks 10.4).
+        // Against an infinite entry of B they are infinite with any sign or NaN, where the first words' sum is what
+        // the whole one would be.
         f32x4 acc[MT][2] = {}, later[2] = {};
         auto add_later = [&](int i) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            acc[i][e / 4][e % 4] = fmaf(later[e / 4][e % 4], 1.0f / kLater, acc[i][e / 4][e % 4]);
+            const float l = fabsf(later[e / 4][e % 4]) < __builtin_inff() ? later[e / 4][e % 4] : 0.0f;
+            acc[i][e / 4][e % 4] = fmaf(l, 1.0f / kLater<DT>, acc[i][e / 4][e % 4]);
           }
         };
         for (int s = 0; s < rp; s += 32) {
@@ -409,14 +413,14 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AdapterArgs a) {
               const u32x4 v = *reinterpret_cast<const u32x4*>(words + w * TR * ld + at);
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                f32x4& to = DT == 0 && w > 0 ? later[h] : acc[i][h];
+                f32x4& to = w > 0 ? later[h] : acc[i][h];
                 to = mfma32<DT>(f[h], v, to);
               }
             }
-            if constexpr (DT == 0 && MT > 1) add_later(i);
+            if constexpr (MT > 1) add_later(i);
           }
         }
-        if constexpr (DT == 0 && MT == 1) add_later(0);
+        if constexpr (MT == 1) add_later(0);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
 #pragma unroll
@@ -566,8 +570,8 @@ hipError_t launch_expand(AdapterArgs a, int cus, hipStream_t st) {
   const auto kernel = expand_kernel<DT, MT, HALF, WHOLE>;
   // A work-group forms the tile's V once for all its columns: so many of them that three work-groups
   // are left for every compute unit, but no more than the rank is worth, since later work-groups even
-  // out what is left at the end (8192 x 11008: rank 128 261 us without that bound, 200 us; rank 16 160
-  // and 140 us; with one block each rank 256 at 4096 x 4096 takes 96 us, not 83).
+  // out what is left at the end (8192 x 11008: rank 128 273 us without that bound, 207 us; rank 16 157
+  // and 142 us; with one block each rank 256 at 4096 x 4096 takes 102 us, not 90).
   const int64_t steps = (a.n + kColumns - 1) / kColumns;
   const int64_t each = std::max<int64_t>(1, std::min<int64_t>({steps, a.tiles * steps / (3 * cus), a.rank / 32}));
   a.blocks = static_cast<int>((steps + each - 1) / each);

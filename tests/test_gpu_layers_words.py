@@ -94,3 +94,29 @@ def test_every_bit_of_the_rank_sums(fl, t, rank, fmt):
     want = 2.0 * V[:, j % rank] * B[0, j, j % rank].double()
     want[::7] = 5.0
     assert torch.equal(Y.double(), want)
+
+
+@pytest.mark.parametrize("t", [5, 1030])
+@pytest.mark.parametrize("fmt", ["bf16", "fp16"])
+@pytest.mark.parametrize("rank", [8, 72])
+def test_infinite_entries_of_the_factor(fl, t, fmt, rank):
+    """Y is infinite, NaN or finite as the sum of the products V B says, whatever words a sum of V takes: sums of
+    one word, of several whose rests have the other sign, and of zero against infinities in B."""
+    k, n, h = 64, 70, HALF[fmt]
+    inf = float("inf")
+    X, A, B = torch.zeros(t, k), torch.zeros(1, rank, k), torch.zeros(1, n, rank)
+    X[:, 0], X[:, 1], X[1::2, 2] = 1.0, 2.0 ** -9, 1.0
+    last = rank - 1
+    A[0, 0, 0] = 1.0                                       # V 1
+    A[0, 3, 0], A[0, 3, 1] = 1.0, 255.0 / 256 * 0.5         # V 1 + 255 / 2^18: its words go up and down
+    A[0, last, 0], A[0, last, 1] = 1.0, -255.0 / 256 * 0.5
+    A[0, 5, 2] = 3.0                                       # V 0 in every other row
+    B[0, 0::7, 0], B[0, 1::7, 3], B[0, 2::7, last], B[0, 3::7, 5] = inf, -inf, inf, inf
+    B[0, 4::7, 0], B[0, 4::7, 3] = inf, -inf
+    B[0, 5::7, 3] = 0.5
+    V = X.double() @ A[0].double().t()
+    want = (V[:, None, :] * B[0].double()[None]).sum(-1)    # 0 times infinity is NaN, as in FP32
+    assert torch.equal(V.float().double(), V) and bool(torch.isnan(want).any()) and bool(torch.isinf(want).any())
+    Y = call(fl, torch.zeros(t, n), X.to(h), A.to(h), B.to(h), torch.zeros(t, dtype=torch.int32), torch.ones(1))
+    assert torch.equal(torch.nan_to_num(Y.double(), nan=7.0, posinf=inf, neginf=-inf),
+                       torch.nan_to_num(want, nan=7.0, posinf=inf, neginf=-inf))
