@@ -14,8 +14,8 @@
 //                              lane four k of one column: no operand is transposed in memory.
 // The activation's operands meet in one lane (gate and up rows take turns in a tile), so H is formed from
 // the accumulators while P is stored, and a verified block costs one pass over X, W, P and H.
-// 4096 x 4096 x 11008 BF16 (P and H): 671 us, 1.10 PFLOP/s; a library product alone takes 693 us there.
-// dX and dW at 2048 x 4096 x 11008: 683 us, 1.08 PFLOP/s (library products 355 and 319 us).
+// 4096 x 4096 x 11008 BF16 (P and H): 668 to 677 us, 1.10 PFLOP/s; a library product alone takes 693 us there.
+// dX and dW at 2048 x 4096 x 11008: 683 to 690 us, 1.07 PFLOP/s (library products 355 and 319 us).
 //
 // Beside it: few_kernel up to 16 tokens; mm_ragged_kernel, the same tiles through registers, where operands off
 // 16-byte groups are not worth the padded copies of pad_kernel; tiny_kernel where an operand has fewer than 8
@@ -417,8 +417,8 @@ __device__ __forceinline__ void stages_ready() {
 // Whole 16-byte groups, two buffers of 64 k: the next step's loads are under way during this one's
 // products.  A buffer is an array of its own, so that the compiler knows loads into one apart from
 // reads of the other.  A step of a 256 x 256 tile takes 1.66 us, a rate of 1.29 PFLOP/s (a library product of 8192
-// x 8192 x 8192 reaches 1.23 to FP32).  By the counters at 4096 x 22016 x 4096 a compute unit has work for 87 % of
-// the launch (6 rounds of work-groups for 5.4), and then its matrix cores are busy for 56 % of the time and LDS for
+// x 8192 x 8192 reaches 1.23 to FP32).  By the counters at 4096 x 22016 x 4096 a compute unit has work for 88 % of
+// the launch (6 rounds of work-groups for 5.4), and then its matrix cores are busy for 57 % of the time and LDS for
 // 21 %, without bank conflicts: no unit is full, the steps wait for their loads at the barriers.  There,
 // loads spread between the products take longer (670 -> 735 us), as do non-temporal stores (674 -> 680)
 // and tiles of the last round in halves (667 -> 676).
